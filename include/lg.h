@@ -16,8 +16,9 @@
  *   - `stream` is a cudaStream_t (0 = default stream).  Calls enqueue work and return;
  *     the return value covers validation and launch only.  A device-side wait that gave
  *     up (every wait in the kernels is bounded) is reported by lg_last_status().
- *   - All tensors are bf16 with the head dimension D contiguous; device pointers must be
- *     16-byte aligned.  Results are bitwise reproducible for fixed inputs and parameters.
+ *   - All tensors are bf16 (the pools of the paged cache: e4m3) with the head dimension D
+ *     contiguous; device pointers must be 16-byte aligned (integer arrays and scales: to their
+ *     element).  Results are bitwise reproducible for fixed inputs and parameters.
  *   - No exception crosses this boundary.  A call with invalid arguments launches nothing.
  */
 #ifndef LG_H_
@@ -37,7 +38,8 @@ typedef enum {
   LG_ERR_WORKSPACE = -3,      /* workspace_bytes smaller than the matching *_workspace_bytes */
   LG_ERR_CUDA = -4,           /* a CUDA runtime / driver call failed                         */
   LG_ERR_DEVICE_TIMEOUT = -5, /* a bounded device-side wait expired (see lg_last_status)     */
-  LG_ERR_ARCH = -6            /* current device is not compute capability 10.x               */
+  LG_ERR_ARCH = -6,           /* current device is not compute capability 10.x               */
+  LG_ERR_PAGE = -7            /* a block table's entry names no page of the pool (see lg_last_status) */
 } lg_status;
 
 typedef enum {
@@ -344,6 +346,104 @@ lg_status lg_sparse_decode_static(const lg_decode_params* p, const void* q, cons
                                   void* stream);
 lg_status lg_sparse_decode_static_reset(void* stream);
 
+/* ---- the cache in 8 bits and in pages ------------------------------------------------- */
+
+/*
+ * The rolling-buffer cache of Section 3.2 for a server whose sequences come and go: the slots of a
+ * sequence are those of the ring above (sink + window; a plain cache of `cap` tokens is sink 0,
+ * window cap), but they are cut into pages of page_tokens slots that lie anywhere in a common pool,
+ * and the tokens are held in 8 bits with one scale per page and kv head.  (The paper has no
+ * counterpart: its rolling buffer is one bf16 array per layer.)
+ *
+ *   k_pool, v_pool   : device [num_pages, Hkv, page_tokens, D] e4m3 (1 byte, 4 significant bits, largest
+ *                      value 448), contiguous, 16-byte aligned.  A value is code * scale.
+ *   k_scale, v_scale : device fp32 [num_pages, Hkv].  lg_paged_append writes powers of two, the smallest one
+ *                      under which the page's largest finite magnitude fits (1 for a page of zeros, never below
+ *                      2^-120); the calls that read take any positive scale.
+ *   block_table      : device int32 [B, table_stride]; slot s of sequence b lies in page
+ *                      block_table[b][s / page_tokens] at offset s % page_tokens.  Entries of pages that hold
+ *                      no token are not read.  An entry that names no page (< 0 or >= num_pages) where a token
+ *                      should be: lg_paged_append drops the token, lg_paged_slot_map answers -1, lg_paged_decode
+ *                      does not attend it, and lg_paged_chunk_prefill writes no result; the last two report
+ *                      LG_ERR_PAGE through lg_last_status() on their workspace.
+ * Several sequences may read the same page; a page that is appended to must belong to one sequence only.
+ * Counts (n_tokens) are 64-bit; a negative one addresses nothing.
+ */
+typedef struct {
+  int32_t B, Hq, Hkv, D;       /* D in {64, 128}; Hq % Hkv == 0                               */
+  int32_t sink_tokens;         /* >= 0                                                       */
+  int32_t window_tokens;       /* >= 1                                                       */
+  int32_t block_tokens;        /* as in lg_decode_params (0: every held token is attended)   */
+  float   scale;               /* softmax scale; 0 selects 1/sqrt(D)                         */
+  int32_t page_tokens;         /* 16, 32, 64 or 128                                          */
+  int32_t num_pages;           /* pages of the pools; num_pages * Hkv * page_tokens < 2^31   */
+  int32_t table_stride;        /* entries per row of block_table, at least
+                                  ceil((sink + window) / page_tokens); 0 selects exactly that */
+} lg_paged_params;
+
+/* Block tables from request lengths: sequence b grows from n_tokens_before[b] (device int64 [B]) by n_new[b] tokens
+ * (device int32 [B]; NULL: T_new for all; values are taken as 0 .. T_new) and needs ceil(min(n, sink + window) /
+ * page_tokens) pages for n tokens.  The pages it lacks are taken from free_pages (device int32 [n_free]) from index
+ * free_start[0] (device int32) on, sequence after sequence, and written into its row of block_table behind the pages
+ * that it has; *free_next (device int32, not free_start) receives the index of the first page that is left.  Where the
+ * list ends before every sequence is served, entries are -1 and *free_next exceeds n_free.  Nothing but these entries
+ * and free_next is written, so the call can be repeated.                                                          */
+lg_status lg_paged_table_extend(const lg_paged_params* p, const int64_t* n_tokens_before, const int32_t* n_new,
+                                int32_t T_new, const int32_t* free_pages, int32_t n_free,
+                                const int32_t* free_start, int32_t* block_table, int32_t* free_next, void* stream);
+
+/* Slot maps: slot_map[b][t] (device int64 [B, T]) = page * page_tokens + offset of the slot that holds the token at
+ * position first[b] + t (device int64 [B]) once n_tokens[b] tokens (device int64 [B]) have been appended; -1 where the
+ * cache does not hold it (overwritten, not there yet, no page) and for t >= count[b] (device int32 [B]; NULL: T).      */
+lg_status lg_paged_slot_map(const lg_paged_params* p, const int64_t* n_tokens, const int64_t* first,
+                            const int32_t* count, int32_t T, const int32_t* block_table, int64_t* slot_map,
+                            void* stream);
+
+/* Append n_new[b] <= T_new tokens per sequence (n_new: device int32 [B] or NULL for T_new; rows behind n_new[b] are not
+ * read): k_new, v_new [B, Hkv, T_new, D] bf16 (device); new_strides: HOST, their strides in elements of (batch, head,
+ * token), multiples of 8, or NULL for contiguous.  Tokens that a later one of the same call would overwrite are not written.
+ * In every page that receives a token the scale becomes that of its tokens, new and kept, and each is rounded to the nearest
+ * code (ties to even; infinities become the largest code, NaN stays NaN, neither counts for the scale).  Kept tokens
+ * change only where the scale does, and then only codes below the normal range (under 2^-6 of the scale) lose bits.  Codes
+ * of slots that hold no token are left as they are.  block_table must name the pages already (lg_paged_table_extend).     */
+lg_status lg_paged_append(const lg_paged_params* p, void* k_pool, void* v_pool, float* k_scale, float* v_scale,
+                          const int32_t* block_table, const void* k_new, const void* v_new,
+                          const int64_t* new_strides, int32_t T_new, const int64_t* n_tokens_before,
+                          const int32_t* n_new, void* stream);
+
+/* Read back: k_out, v_out [B, Hkv, T, D] bf16 (device, contiguous) = the rows at slot_map[b][t] (device int64 [B, T], as
+ * lg_paged_slot_map writes it; any order, repeats allowed); zeros where it is negative or beyond the pool.  Exact for the
+ * scales that lg_paged_append writes.                                                                                */
+lg_status lg_paged_gather(const lg_paged_params* p, const void* k_pool, const void* v_pool, const float* k_scale,
+                          const float* v_scale, const int64_t* slot_map, int32_t T, void* k_out, void* v_out,
+                          void* stream);
+
+/* lg_sparse_decode over the paged cache: q [B,Hq,D], o [B,Hq,D] bf16, lse [B,Hq] fp32 (NULL to skip), n_tokens (device
+ * int64 [B]) counts the tokens appended so far, the current one included.  Scores and outputs are computed from the codes
+ * without further rounding of K, V or q (but for elements of a row of q below 2^-24 of its largest); the weights are
+ * rounded to f16, their sum is not.  workspace: device, 256-byte aligned, lg_paged_decode_workspace_bytes() bytes (0 = invalid
+ * arguments), zero-filled once by lg_sparse_decode_workspace_init(); two calls that can run at the same time (two captured
+ * graphs too) need a workspace each.                                                                                 */
+size_t lg_paged_decode_workspace_bytes(const lg_paged_params* p);
+lg_status lg_paged_decode(const lg_paged_params* p, const void* q, const void* k_pool, const void* v_pool,
+                          const float* k_scale, const float* v_scale, const int32_t* block_table,
+                          const int64_t* n_tokens, void* o, float* lse, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/* lg_chunk_prefill over the paged cache: T new tokens of every sequence attend to what its cache holds and, causally, to
+ * themselves (the chunk's own k_chunk, v_chunk as given, in bf16: they are rounded when they are appended, afterwards, by
+ * lg_paged_append).  n_tokens_before: HOST int64 [B], >= 0 each; neighbouring sequences that keep the same number of
+ * tokens are worked together.  sink_tokens and window_tokens are multiples of 64, window_tokens >= 64.  The cache is
+ * copied in bf16 and in time order into the workspace (device, 256-byte aligned,
+ * lg_paged_chunk_prefill_workspace_bytes() bytes), and the forward kernel runs over it.  A failure of any of the
+ * launches is reported by lg_last_status(workspace, stream).                                                         */
+size_t lg_paged_chunk_prefill_workspace_bytes(const lg_paged_params* p, int32_t T, const int64_t* n_tokens_before);
+lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, const void* k_chunk,
+                                 const void* v_chunk, const void* k_pool, const void* v_pool, const float* k_scale,
+                                 const float* v_scale, const int32_t* block_table, int32_t T,
+                                 const int64_t* n_tokens_before, void* o, float* lse, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
 /* ---- self-test of the error path -------------------------------------------------------- */
 
 /* (The paper has no counterpart; this exists so that the error path can be exercised without
@@ -362,7 +462,8 @@ lg_status lg_selftest_wait_timeout(void* workspace, void* stream);
  * `workspace` (attention or decode workspace) and clears them.  LG_OK;
  * LG_ERR_DEVICE_TIMEOUT if a bounded wait expired in a kernel that used the workspace since
  * the last call of this function (a later call on the same workspace does not hide it);
- * LG_ERR_WORKSPACE if a call with lists_prepared = 1 found lists of another pattern.       */
+ * LG_ERR_WORKSPACE if a call with lists_prepared = 1 found lists of another pattern; LG_ERR_PAGE if
+ * a call over the paged cache met a table entry that names no page.                        */
 lg_status lg_last_status(void* workspace, void* stream);
 
 const char* lg_status_string(lg_status s);

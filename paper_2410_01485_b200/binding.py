@@ -47,6 +47,13 @@ class DecodeParams(C.Structure):
                 ("scale", C.c_float)]
 
 
+class PagedParams(C.Structure):
+    _fields_ = [("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
+                ("sink_tokens", C.c_int32), ("window_tokens", C.c_int32), ("block_tokens", C.c_int32),
+                ("scale", C.c_float), ("page_tokens", C.c_int32), ("num_pages", C.c_int32),
+                ("table_stride", C.c_int32)]
+
+
 _lib = None
 
 # every symbol include/lg.h declares: (restype, argtypes)
@@ -72,6 +79,14 @@ SYMBOLS = {
                                    _vp, _sz, _vp]),
     "lg_sparse_decode_static": (C.c_int, [C.POINTER(DecodeParams), _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "lg_sparse_decode_static_reset": (C.c_int, [_vp]),
+    "lg_paged_table_extend": (C.c_int, [C.POINTER(PagedParams), _vp, _vp, C.c_int32, _vp, C.c_int32, _vp, _vp, _vp, _vp]),
+    "lg_paged_slot_map": (C.c_int, [C.POINTER(PagedParams), _vp, _vp, _vp, C.c_int32, _vp, _vp, _vp]),
+    "lg_paged_append": (C.c_int, [C.POINTER(PagedParams)] + [_vp] * 8 + [C.c_int32, _vp, _vp, _vp]),
+    "lg_paged_gather": (C.c_int, [C.POINTER(PagedParams)] + [_vp] * 5 + [C.c_int32, _vp, _vp, _vp]),
+    "lg_paged_decode_workspace_bytes": (_sz, [C.POINTER(PagedParams)]),
+    "lg_paged_decode": (C.c_int, [C.POINTER(PagedParams)] + [_vp] * 10 + [_sz, _vp]),
+    "lg_paged_chunk_prefill_workspace_bytes": (_sz, [C.POINTER(PagedParams), C.c_int32, _vp]),
+    "lg_paged_chunk_prefill": (C.c_int, [C.POINTER(PagedParams)] + [_vp] * 8 + [C.c_int32] + [_vp] * 4 + [_sz, _vp]),
     "lg_selftest_wait_timeout": (C.c_int, [_vp, _vp]),
     "lg_last_status": (C.c_int, [_vp, _vp]),
     "lg_status_string": (C.c_char_p, [C.c_int]),
@@ -411,6 +426,199 @@ def lg_sparse_decode_static(p: DecodeParams, q, k_cache, v_cache, n_tokens, o, l
                                                   n_tokens.data_ptr(), o.data_ptr(),
                                                   lse.data_ptr() if lse is not None else None, _stream()),
            "lg_sparse_decode_static")
+    return o, lse
+
+
+# ------------------------------------------------------------------------- paged 8-bit cache
+
+def paged_params(B, Hq, Hkv, D, sink_tokens, window_tokens, page_tokens, num_pages, scale=0.0, block_tokens=0,
+                 table_stride=0) -> PagedParams:
+    """Pools are float8_e4m3fn (or uint8) tensors [num_pages, Hkv, page_tokens, D], scales fp32 [num_pages, Hkv], the
+    block table int32 [B, table_stride] (table_stride 0: ceil((sink_tokens + window_tokens) / page_tokens))."""
+    return PagedParams(B, Hq, Hkv, D, sink_tokens, window_tokens, block_tokens, scale, page_tokens, num_pages, table_stride)
+
+
+def _check_cache(p: PagedParams, k_pool, v_pool, k_scale, v_scale, block_table):
+    for pool in (k_pool, v_pool):
+        assert pool.dtype in (torch.float8_e4m3fn, torch.uint8) and pool.is_contiguous()
+        assert tuple(pool.shape) == (p.num_pages, p.Hkv, p.page_tokens, p.D)
+    for s in (k_scale, v_scale):
+        assert s.dtype == torch.float32 and s.is_contiguous() and tuple(s.shape) == (p.num_pages, p.Hkv)
+    if block_table is not None:
+        _check_table(p, block_table)
+
+
+def _check_table(p: PagedParams, block_table):
+    columns = p.table_stride or -(-(p.sink_tokens + p.window_tokens) // max(1, p.page_tokens))
+    assert block_table.dtype == torch.int32 and block_table.is_contiguous() and tuple(block_table.shape) == (p.B, columns)
+
+
+def _check_counts(p: PagedParams, dtype, *counts):
+    for n in counts:
+        assert n is None or (n.dtype == dtype and n.is_contiguous() and n.numel() == p.B)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def lg_paged_table_extend(p: PagedParams, n_tokens_before, n_new, free_pages, free_start, block_table, free_next,
+                          T_new: Optional[int] = None):
+    """New pages from free_pages (int32) into block_table for sequences that grow from n_tokens_before (int64 [B]) by n_new
+    (int32 [B]; None: T_new each) tokens; free_start, free_next: int32 tensors of one element each."""
+    assert n_new is not None or T_new is not None
+    _check_counts(p, torch.int64, n_tokens_before)
+    _check_counts(p, torch.int32, n_new)
+    _check_table(p, block_table)
+    assert free_pages.dtype == free_start.dtype == free_next.dtype == torch.int32 and free_pages.is_contiguous()
+    _check(load_library().lg_paged_table_extend(
+        C.byref(p), n_tokens_before.data_ptr(), _ptr(n_new), 0x7fffffff if T_new is None else T_new, free_pages.data_ptr(),
+        free_pages.numel(), free_start.data_ptr(), block_table.data_ptr(), free_next.data_ptr(), _stream()),
+        "lg_paged_table_extend")
+
+
+def lg_paged_slot_map(p: PagedParams, n_tokens, first, count, block_table, slot_map):
+    """slot_map (int64 [B, T]): where the cache holds positions first .. first + count - 1 (count int32 [B]; None: T)."""
+    _check_counts(p, torch.int64, n_tokens, first)
+    _check_counts(p, torch.int32, count)
+    _check_table(p, block_table)
+    assert slot_map.dtype == torch.int64 and slot_map.is_contiguous() and slot_map.shape[0] == p.B
+    _check(load_library().lg_paged_slot_map(C.byref(p), n_tokens.data_ptr(), first.data_ptr(), _ptr(count), slot_map.shape[1],
+                                            block_table.data_ptr(), slot_map.data_ptr(), _stream()), "lg_paged_slot_map")
+    return slot_map
+
+
+def _append_args(p: PagedParams, k_pool, v_pool, k_scale, v_scale, block_table, k_new, v_new, n_tokens_before, n_new):
+    _check_cache(p, k_pool, v_pool, k_scale, v_scale, block_table)
+    _check_counts(p, torch.int64, n_tokens_before)
+    _check_counts(p, torch.int32, n_new)
+    shape = tuple(k_new.shape)
+    assert len(shape) == 4 and shape[:2] == (p.B, p.Hkv) and shape[3] == p.D and tuple(v_new.shape) == shape
+    assert k_new.dtype == v_new.dtype == torch.bfloat16
+    whole = (p.Hkv * shape[2] * p.D, shape[2] * p.D, p.D)
+    strides = []
+    for t in (k_new, v_new):   # (the stride of a dimension of one element says nothing)
+        assert t.stride(3) == 1 or shape[2] == 0, "expect contiguous D"
+        strides.append(tuple(w if n == 1 else s for s, n, w in zip(t.stride(), shape, whole)))
+    assert strides[0] == strides[1], "k_new and v_new must have the same strides"
+    st = None if strides[0] == whole else (C.c_int64 * 3)(*strides[0])
+    return (C.byref(p), k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(),
+            k_new.data_ptr(), v_new.data_ptr(), st, shape[2], n_tokens_before.data_ptr(), _ptr(n_new))
+
+
+def lg_paged_append(p: PagedParams, k_pool, v_pool, k_scale, v_scale, block_table, k_new, v_new, n_tokens_before, n_new=None):
+    """Append k_new, v_new [B,Hkv,T,D] (any strides of 8 elements with contiguous D) in place; n_tokens_before int64 [B], n_new
+    int32 [B] or None for T tokens each."""
+    _check(load_library().lg_paged_append(*_append_args(p, k_pool, v_pool, k_scale, v_scale, block_table, k_new, v_new,
+                                                        n_tokens_before, n_new), _stream()), "lg_paged_append")
+
+
+def paged_append_call(p: PagedParams, k_pool, v_pool, k_scale, v_scale, block_table, k_new, v_new, n_tokens_before, n_new=None,
+                      stream=None):
+    """lg_paged_append on fixed buffers, every argument marshalled once (as decode_call)."""
+    args = _append_args(p, k_pool, v_pool, k_scale, v_scale, block_table, k_new, v_new, n_tokens_before, n_new)
+    return _fixed_call("lg_paged_append", args, stream,
+                       (p, k_pool, v_pool, k_scale, v_scale, block_table, k_new, v_new, n_tokens_before, n_new))
+
+
+def lg_paged_gather(p: PagedParams, k_pool, v_pool, k_scale, v_scale, slot_map, k_out=None, v_out=None):
+    """Rows of the cache at slot_map (int64 [B, T]) as bf16 [B, Hkv, T, D]; zeros where it is negative."""
+    _check_cache(p, k_pool, v_pool, k_scale, v_scale, None)
+    assert slot_map.dtype == torch.int64 and slot_map.is_contiguous() and slot_map.shape[0] == p.B
+    T = slot_map.shape[1]
+    if k_out is None:
+        k_out = torch.empty(p.B, p.Hkv, T, p.D, dtype=torch.bfloat16, device=k_pool.device)
+    if v_out is None:
+        v_out = torch.empty_like(k_out)
+    for t in (k_out, v_out):
+        assert t.dtype == torch.bfloat16 and t.is_contiguous() and tuple(t.shape) == (p.B, p.Hkv, T, p.D)
+    _check(load_library().lg_paged_gather(C.byref(p), k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                                          slot_map.data_ptr(), T, k_out.data_ptr(), v_out.data_ptr(), _stream()), "lg_paged_gather")
+    return k_out, v_out
+
+
+def paged_decode_workspace(p: PagedParams, device="cuda") -> torch.Tensor:
+    """A workspace ready for lg_paged_decode (allocated and zero-filled)."""
+    n = load_library().lg_paged_decode_workspace_bytes(C.byref(p))
+    if n == 0:
+        raise LgError(-1, "lg_paged_decode_workspace_bytes")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    _check(load_library().lg_sparse_decode_workspace_init(ws.data_ptr(), ws.numel(), _stream()),
+           "lg_sparse_decode_workspace_init")
+    return ws
+
+
+def _decode_args(p: PagedParams, q, k_pool, v_pool, k_scale, v_scale, block_table, n_tokens, o, lse, workspace):
+    _check_cache(p, k_pool, v_pool, k_scale, v_scale, block_table)
+    _check_counts(p, torch.int64, n_tokens)
+    for t in (q, o):
+        assert t.dtype == torch.bfloat16 and t.is_contiguous() and tuple(t.shape) == (p.B, p.Hq, p.D)
+    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (p.B, p.Hq))
+    return (C.byref(p), q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+            block_table.data_ptr(), n_tokens.data_ptr(), o.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel())
+
+
+def lg_paged_decode(p: PagedParams, q, k_pool, v_pool, k_scale, v_scale, block_table, n_tokens, o=None, lse=None, workspace=None,
+                    want_lse: bool = True):
+    """q [B,Hq,D] bf16 over the paged cache -> (o [B,Hq,D] bf16, lse [B,Hq] fp32 or None)."""
+    o = torch.empty_like(q) if o is None else o
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    ws = paged_decode_workspace(p, q.device) if workspace is None else workspace
+    _check(load_library().lg_paged_decode(*_decode_args(p, q, k_pool, v_pool, k_scale, v_scale, block_table, n_tokens, o, lse, ws),
+                                          _stream()), "lg_paged_decode")
+    return o, lse
+
+
+def paged_decode_call(p: PagedParams, q, k_pool, v_pool, k_scale, v_scale, block_table, n_tokens, o, lse, workspace, stream=None):
+    """lg_paged_decode on fixed buffers, every argument marshalled once (as decode_call)."""
+    args = _decode_args(p, q, k_pool, v_pool, k_scale, v_scale, block_table, n_tokens, o, lse, workspace)
+    return _fixed_call("lg_paged_decode", args, stream,
+                       (p, q, k_pool, v_pool, k_scale, v_scale, block_table, n_tokens, o, lse, workspace))
+
+
+def _fixed_call(name, args, stream, keep):
+    """A function without arguments that makes the call on `stream` (default: the one current now); `keep` stays alive."""
+    fn = getattr(load_library(), name)
+    handle = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    args = tuple(t(a) if isinstance(a, int) else a for t, a in zip(fn.argtypes, args)) + (C.c_void_p(handle),)
+
+    def call(_keep=keep):
+        code = fn(*args)
+        if code != LG_OK:
+            raise LgError(code, name)
+
+    return call
+
+
+def _host_counts(p: PagedParams, n_tokens_before):
+    n = [int(x) for x in n_tokens_before]
+    assert len(n) == p.B
+    return (C.c_int64 * p.B)(*n)
+
+
+def paged_chunk_prefill_workspace(p: PagedParams, T: int, n_tokens_before, device="cuda") -> torch.Tensor:
+    n = load_library().lg_paged_chunk_prefill_workspace_bytes(C.byref(p), T, _host_counts(p, n_tokens_before))
+    if n == 0:
+        raise LgError(-1, "lg_paged_chunk_prefill_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def lg_paged_chunk_prefill(p: PagedParams, q_chunk, k_chunk, v_chunk, k_pool, v_pool, k_scale, v_scale, block_table, n_tokens_before,
+                           o=None, lse=None, workspace=None):
+    """q_chunk [B,Hq,T,D], k_chunk, v_chunk [B,Hkv,T,D] bf16 against the paged cache; n_tokens_before: B host integers.
+    Returns (o [B,Hq,T,D] bf16, lse [B,Hq,T] fp32)."""
+    _check_cache(p, k_pool, v_pool, k_scale, v_scale, block_table)
+    T = q_chunk.shape[2]
+    for t, H in ((q_chunk, p.Hq), (k_chunk, p.Hkv), (v_chunk, p.Hkv)):
+        assert t.dtype == torch.bfloat16 and t.is_contiguous() and tuple(t.shape) == (p.B, H, T, p.D)
+    o = torch.empty_like(q_chunk) if o is None else o
+    lse = torch.empty(q_chunk.shape[:3], dtype=torch.float32, device=q_chunk.device) if lse is None else lse
+    ws = paged_chunk_prefill_workspace(p, T, n_tokens_before, q_chunk.device) if workspace is None else workspace
+    _check(load_library().lg_paged_chunk_prefill(
+        C.byref(p), q_chunk.data_ptr(), k_chunk.data_ptr(), v_chunk.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
+        k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(), T, _host_counts(p, n_tokens_before), o.data_ptr(),
+        lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream()), "lg_paged_chunk_prefill")
     return o, lse
 
 

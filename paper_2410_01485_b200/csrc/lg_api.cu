@@ -325,6 +325,16 @@ lg_status make_tmap(CUtensorMap* out, const void* base, int B, int H, int L, int
   return rc == CUDA_SUCCESS ? LG_OK : LG_ERR_CUDA;
 }
 
+// rows of bytes (the element type does not matter to a copy)
+lg_status encode_tmap_u8(CUtensorMap* out, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
+                         CUtensorMapSwizzle swizzle) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return LG_ERR_CUDA;
+  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  CUresult rc = fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return rc == CUDA_SUCCESS ? LG_OK : LG_ERR_CUDA;
+}
 
 // ---- chunk served against a sink + window ring ----------------------------------------------
 struct ChunkPlan {
@@ -631,6 +641,98 @@ lg_status lg_chunk_prefill(const lg_decode_params* p, const void* q_chunk, const
   return launch_fwd(c.r, c.w, q_chunk, k_lin, v_lin, o, lse, ws, st);
 }
 
+// The sequences are taken in runs of neighbours that keep as many tokens (and, with a block-aligned window, have the same phase): the
+// attention kernel's rows are counted from the number of kept tokens.  Rings that are full, and a batch at one position, are one run.
+namespace {
+lg_decode_params ring_of(const lg_paged_params* p, int B) {
+  lg_decode_params d;
+  d.B = B; d.Hq = p->Hq; d.Hkv = p->Hkv; d.D = p->D;
+  d.sink_tokens = p->sink_tokens; d.window_tokens = p->window_tokens; d.block_tokens = p->block_tokens; d.scale = p->scale;
+  return d;
+}
+int chunk_run(const lg_paged_params* p, const int64_t* n, int b) {   // end of the run that starts at sequence b
+  const int64_t cap = static_cast<int64_t>(p->sink_tokens) + p->window_tokens;
+  auto same = [&](int64_t x, int64_t y) {
+    if ((x < cap ? x : cap) != (y < cap ? y : cap)) return false;
+    return p->block_tokens <= 0 || x < cap || (x - cap) % p->block_tokens == (y - cap) % p->block_tokens;
+  };
+  int e = b + 1;
+  while (e < p->B && same(n[b], n[e])) ++e;
+  return e;
+}
+lg_status paged_chunk_bytes(const lg_paged_params* p, int32_t T, const int64_t* n, size_t* total) {
+  const lg_status s = check_paged(p);
+  if (s != LG_OK) return s;
+  if (!n) return LG_ERR_INVALID_ARG;
+  *total = 0;
+  for (int b = 0; b < p->B;) {
+    const int e = chunk_run(p, n, b);
+    const lg_decode_params d = ring_of(p, e - b);
+    ChunkPlan c;
+    const lg_status r = plan_chunk(&d, T, n[b], &c);
+    if (r != LG_OK) return r;
+    if (c.total > *total) *total = c.total;
+    b = e;
+  }
+  return LG_OK;
+}
+}  // namespace
+
+size_t lg_paged_chunk_prefill_workspace_bytes(const lg_paged_params* p, int32_t T, const int64_t* n_tokens_before) {
+  size_t total = 0;
+  return paged_chunk_bytes(p, T, n_tokens_before, &total) == LG_OK ? total : 0;
+}
+
+lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, const void* k_chunk, const void* v_chunk, const void* k_pool,
+                                 const void* v_pool, const float* k_scale, const float* v_scale, const int32_t* block_table, int32_t T,
+                                 const int64_t* n_tokens_before, void* o, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  LG_RANGE("lg_paged_chunk_prefill");
+  size_t total = 0;
+  lg_status s = paged_chunk_bytes(p, T, n_tokens_before, &total);
+  if (s != LG_OK) return s;
+  if (!q_chunk || !k_chunk || !v_chunk || !k_pool || !v_pool || !k_scale || !v_scale || !block_table || !o || !lse || !workspace)
+    return LG_ERR_INVALID_ARG;
+  if (!aligned16(q_chunk) || !aligned16(k_chunk) || !aligned16(v_chunk) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(o) ||
+      !aligned16(lse) || ((reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale) | reinterpret_cast<uintptr_t>(block_table)) & 3) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255))
+    return LG_ERR_INVALID_ARG;
+  if (workspace_bytes < total) return LG_ERR_WORKSPACE;
+  if ((s = check_arch()) != LG_OK) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const int stride = paged_table_stride(p);
+  for (int b = 0; b < p->B;) {
+    const int e = chunk_run(p, n_tokens_before, b);
+    const int64_t n = n_tokens_before[b], q_at = static_cast<int64_t>(b) * p->Hq * T;
+    const lg_decode_params d = ring_of(p, e - b);
+    ChunkPlan c;
+    if ((s = plan_chunk(&d, T, n, &c)) != LG_OK) return s;
+    if ((s = prepare_workspace(c.r, c.w, ws, 1, true, 0, st)) != LG_OK) return s;
+    PagedLinearise l;
+    l.pool[0] = k_pool; l.pool[1] = v_pool; l.scale[0] = k_scale; l.scale[1] = v_scale;
+    l.error_word = reinterpret_cast<unsigned int*>(ws);
+    l.Hkv = p->Hkv; l.D = p->D; l.T = T; l.kept = c.kept; l.sink = p->sink_tokens; l.window = p->window_tokens;
+    l.page_shift = page_shift(p->page_tokens); l.num_pages = p->num_pages; l.stride = stride;
+    __nv_bfloat16* lin[2] = {reinterpret_cast<__nv_bfloat16*>(ws + c.o_k), reinterpret_cast<__nv_bfloat16*>(ws + c.o_v)};
+    for (int x = b; x < e; x += kLineariseSeqs) {
+      const int m = e - x < kLineariseSeqs ? e - x : kLineariseSeqs;
+      for (int y = 0; y < m; ++y)
+        l.ring0[y] = c.kept > p->sink_tokens ? static_cast<int>((n_tokens_before[x + y] - c.kept) % p->window_tokens) : 0;
+      for (int y = 0; y < 2; ++y) {
+        l.chunk[y] = static_cast<const __nv_bfloat16*>(y ? v_chunk : k_chunk) + static_cast<int64_t>(x) * p->Hkv * T * p->D;
+        l.lin[y] = lin[y] + static_cast<int64_t>(x - b) * p->Hkv * c.ap.L * p->D;
+      }
+      l.table = block_table + static_cast<int64_t>(x) * stride;
+      if ((s = launch_paged_linearise(l, m, st)) != LG_OK) return s;
+    }
+    if ((s = launch_fwd(c.r, c.w, static_cast<const __nv_bfloat16*>(q_chunk) + q_at * p->D, lin[0], lin[1],
+                        static_cast<__nv_bfloat16*>(o) + q_at * p->D, lse + q_at, ws, st)) != LG_OK)
+      return s;
+    b = e;
+  }
+  return LG_OK;
+}
+
 lg_status lg_selftest_wait_timeout(void* workspace, void* stream) {
   LG_RANGE("lg_selftest_wait_timeout");
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255)) return LG_ERR_INVALID_ARG;
@@ -654,6 +756,7 @@ lg_status lg_last_status(void* workspace, void* stream) {
     const unsigned int first = word[1] != 0 ? word[1] : word[0];
     // 3: lists of another pattern; 4 (checked builds): a schedule value out of range -- either way the workspace is not
     // what the call needs
+    if ((first >> 24) == 5u) return LG_ERR_PAGE;
     return ((first >> 24) == 3u || (first >> 24) == 4u) ? LG_ERR_WORKSPACE : LG_ERR_DEVICE_TIMEOUT;
   }
   return LG_OK;
@@ -670,6 +773,7 @@ const char* lg_status_string(lg_status s) {
     case LG_ERR_CUDA: return "CUDA call failed";
     case LG_ERR_DEVICE_TIMEOUT: return "a bounded device-side wait expired";
     case LG_ERR_ARCH: return "device is not sm_100";
+    case LG_ERR_PAGE: return "a block table's entry names no page of the pool";
   }
   return "unknown status";
 }

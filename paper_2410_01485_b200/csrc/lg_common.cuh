@@ -11,7 +11,8 @@ namespace lg {
 struct WsHeader {
   unsigned int error_word;         // 0 = ok; else (code << 24) | site.  code 1: a wait gave up, 2: shared memory
                                    // misaligned, 3: the workspace does not hold the lists the call was told it holds,
-                                   // 4: a schedule value out of range (checked builds only)
+                                   // 4: a schedule value out of range (checked builds only), 5: a block table's entry
+                                   // that names no page of the pool
   unsigned int latched;            // an error word that a later call found unread and kept for lg_last_status
   unsigned long long magic;        // kWsMagic once the header has been initialised by a call
   unsigned long long fingerprint;  // which pattern the lists and schedules below were built for (0: none)
@@ -27,8 +28,9 @@ struct __align__(16) TileRec {
 constexpr int kDqEntInts = 5;   // ints per entry of the schedule of the dQ pass that reads dS back (dq_entries)
 constexpr unsigned long long kWsMagic = 0x4c47575348445231ull;   // "LGWSHDR1"
 static_assert(sizeof(WsHeader) == 256, "header size");
-// a word that a kernel can have left (0 included): a code of 1 to 4 and a site
-__device__ __forceinline__ bool is_status(unsigned int w) { return w == 0 || ((w >> 24) >= 1 && (w >> 24) <= 4 && (w & 0xffffffu) < 256); }
+constexpr unsigned int kPageError = (5u << 24) | 1u;
+// a word that a kernel can have left (0 included): a code of 1 to 5 and a site
+__device__ __forceinline__ bool is_status(unsigned int w) { return w == 0 || ((w >> 24) >= 1 && (w >> 24) <= 5 && (w & 0xffffffu) < 256); }
 
 // A call that was told its workspace holds prepared lists checks, before it reads any of them,
 // that the header carries a fingerprint it accepts; otherwise the CTA records code 3 and returns.

@@ -211,4 +211,23 @@ lg_status attn_bwd_entry(const lg_attn_params* p, const void* q, const void* k, 
                          int kv_total = 0 /* the same */);
 size_t attn_workspace_bytes(const lg_attn_params* p, int want_bwd, int kv_total);
 
+// ---- paged 8-bit cache (lg_paged.cu)
+lg_status check_paged(const lg_paged_params* p);
+int paged_table_stride(const lg_paged_params* p);
+int page_shift(int page_tokens);
+lg_status encode_tmap_u8(CUtensorMap* out, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
+                         CUtensorMapSwizzle swizzle);
+constexpr int kLineariseSeqs = 128;   // sequences of one launch
+struct PagedLinearise {
+  const void* pool[2];       // K, V
+  const float* scale[2];
+  const void* chunk[2];      // [B, Hkv, T, D] bf16
+  void* lin[2];              // [B, Hkv, kept + T, D] bf16
+  const int32_t* table;
+  unsigned int* error_word;
+  int Hkv, D, T, kept, sink, window, page_shift, num_pages, stride;
+  int ring0[kLineariseSeqs]; // ring offset of each sequence's oldest kept token
+};
+lg_status launch_paged_linearise(const PagedLinearise& a, int B /* <= kLineariseSeqs */, cudaStream_t stream);
+
 }  // namespace lg

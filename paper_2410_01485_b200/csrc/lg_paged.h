@@ -1,0 +1,87 @@
+// Index arithmetic of the paged cache, shared by the host and the kernels.  The slots of a sequence are those of the
+// rolling-buffer ring (paper Section 3.2): token j lives in slot j < sink ? j : sink + (j - sink) % window, and the
+// sink + window slots are cut into pages of page_tokens each.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace lg {
+
+// Smallest exponent of a page's scale: its inverse and the scale itself stay normal fp32 numbers (the largest one, for the
+// largest bf16, is 2^120).  Values that would need a smaller one are below 2^-111 and become small codes or zeros.
+constexpr int kPageMinExp = -120;
+constexpr int kPageMaxTokens = 128;
+
+__host__ __device__ __forceinline__ int slot_of(int64_t pos, int sink, int window) {
+  return static_cast<int>(pos < sink ? pos : sink + (pos - sink) % window);
+}
+
+// position of the token that `slot` holds once n tokens have been appended, -1: none yet
+__host__ __device__ __forceinline__ int64_t held_position(int64_t slot, int64_t n, int sink, int window) {
+  if (slot >= n || slot >= static_cast<int64_t>(sink) + window) return -1;
+  return slot < sink ? slot : slot + (n - 1 - slot) / window * window;
+}
+
+// pages that the cache of a sequence of n tokens takes (n < 0 counts as 0)
+__host__ __device__ __forceinline__ int pages_of(int64_t n, int sink, int window, int page_tokens) {
+  const int64_t cap = static_cast<int64_t>(sink) + window, held = n < 0 ? 0 : n < cap ? n : cap;
+  return static_cast<int>((held + page_tokens - 1) / page_tokens);
+}
+
+// The pages that a call writes which takes a sequence from n0 to n1 tokens: the slots of the new tokens are up to three
+// runs (in the sink; in the ring from its start, if the call wraps around; in the ring up to its end), listed here by
+// ascending page, no page twice.
+struct TouchedPages {
+  int first[3], count[3];
+  __host__ __device__ __forceinline__ int total() const { return count[0] + count[1] + count[2]; }
+  __host__ __device__ __forceinline__ int page(int i) const {   // 0 <= i < total()
+    if (i < count[0]) return first[0] + i;
+    i -= count[0];
+    if (i < count[1]) return first[1] + i;
+    return first[2] + i - count[1];
+  }
+};
+__host__ __device__ __forceinline__ TouchedPages touched_pages(int64_t n0, int64_t n1, int sink, int window, int page_tokens) {
+  int64_t from[3] = {0, 0, 0}, to[3] = {0, 0, 0};              // slot runs [from, to)
+  if (n0 < sink) { from[0] = n0; to[0] = n1 < sink ? n1 : sink; }
+  const int64_t start = n0 > sink ? n0 : sink;                 // first new token of the ring
+  if (n1 > start) {
+    const int64_t m = n1 - start < window ? n1 - start : window;   // those of them that survive the call
+    const int64_t r0 = (n1 - m - sink) % window;
+    if (r0 + m <= window) {
+      from[2] = sink + r0; to[2] = sink + r0 + m;
+    } else {
+      from[2] = sink + r0; to[2] = static_cast<int64_t>(sink) + window;
+      from[1] = sink; to[1] = sink + r0 + m - window;
+    }
+  }
+  TouchedPages t;
+  int64_t next = 0;                                            // first page not listed yet
+  for (int i = 0; i < 3; ++i) {
+    int64_t a = from[i] / page_tokens, b = to[i] > from[i] ? (to[i] - 1) / page_tokens + 1 : a;
+    if (a < next) a = next;
+    if (b < a) b = a;
+    t.first[i] = static_cast<int>(a);
+    t.count[i] = static_cast<int>(b - a);
+    if (b > a) next = b;
+  }
+  return t;
+}
+// no call of up to T tokens a sequence touches more pages than this (a run of m slots lies in at most m / P + 2 pages)
+__host__ __device__ __forceinline__ int max_touched_pages(int64_t T, int sink, int window, int page_tokens) {
+  const int64_t all = (static_cast<int64_t>(sink) + window + page_tokens - 1) / page_tokens;
+  int64_t n = T / page_tokens + 6;
+  if (n > T) n = T;
+  return static_cast<int>(n < all ? n : all);
+}
+
+// Exponent of the smallest power-of-two scale under which a value of magnitude `amax` (finite, >= 0) fits e4m3, whose
+// largest number is 448 = 1.75 * 2^8.
+__host__ __device__ __forceinline__ int page_exponent(uint32_t amax_bits /* of the fp32 value */) {
+  if (amax_bits == 0) return 0;
+  const int biased = static_cast<int>(amax_bits >> 23);        // 0: subnormal, clamped below like all that small
+  const int e = biased - 127 - 8 + ((amax_bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return e < kPageMinExp ? kPageMinExp : e;
+}
+
+}  // namespace lg
