@@ -325,16 +325,6 @@ lg_status make_tmap(CUtensorMap* out, const void* base, int B, int H, int L, int
   return rc == CUDA_SUCCESS ? LG_OK : LG_ERR_CUDA;
 }
 
-// rows of bytes (the element type does not matter to a copy)
-lg_status encode_tmap_u8(CUtensorMap* out, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
-                         CUtensorMapSwizzle swizzle) {
-  EncodeTiledFn fn = get_encode_fn();
-  if (!fn) return LG_ERR_CUDA;
-  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-  CUresult rc = fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                   swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return rc == CUDA_SUCCESS ? LG_OK : LG_ERR_CUDA;
-}
 
 // ---- chunk served against a sink + window ring ----------------------------------------------
 struct ChunkPlan {

@@ -215,8 +215,6 @@ size_t attn_workspace_bytes(const lg_attn_params* p, int want_bwd, int kv_total)
 lg_status check_paged(const lg_paged_params* p);
 int paged_table_stride(const lg_paged_params* p);
 int page_shift(int page_tokens);
-lg_status encode_tmap_u8(CUtensorMap* out, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
-                         CUtensorMapSwizzle swizzle);
 constexpr int kLineariseSeqs = 128;   // sequences of one launch
 struct PagedLinearise {
   const void* pool[2];       // K, V

@@ -6,7 +6,6 @@
 // rescaled by exponents alone, which is exact but for codes below the normal range (values under 2^-14 of the largest),
 // where scales of amax / 448 would round every token of the page anew with every append.  e4m3 keeps 4 significant bits
 // wherever a value lies in its 15 octaves, so nothing is lost by a scale up to twice as large.
-#include <cuda.h>
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -129,7 +128,7 @@ __global__ void __launch_bounds__(kSlotMapThreads) slot_map_kernel(const SlotMap
   int64_t out = -1;
   if (t < new_tokens(a.count, b, a.T) && pos >= 0 && pos < n) {
     const int slot = slot_of(pos, a.sink, a.window);
-    if (held_position(slot, n, a.sink, a.window) == pos) {
+    if (held_position(slot, n, ring_head(n, a.sink, a.window), a.sink, a.window) == pos) {
       const int page = checked_page(a.table[static_cast<int64_t>(b) * a.stride + (slot >> a.page_shift)], a.num_pages);
       if (page >= 0) out = (static_cast<int64_t>(page) << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
     }
@@ -150,11 +149,11 @@ struct AppendArgs {
   const int64_t* n_before;
   const int32_t* n_new;      // or null
   int64_t stride_b, stride_h, stride_t;
-  int B, Hkv, T, sink, window, page_tokens, num_pages, stride, max_touched;
+  int B, Hkv, T, sink, window, page_shift, num_pages, stride, max_touched;
 };
 constexpr int kAppendThreads = 128;
 
-template <int D, int NU>     // NU units of 8 elements a thread: page_tokens = NU * 8 * kAppendThreads / D
+template <int D, int NU, bool kOne>   // NU units of 8 elements a thread: page_tokens = NU * 8 * kAppendThreads / D; kOne: one token at most
 __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const AppendArgs a) {
   pdl_trigger();
   constexpr int kPerRow = D / 8, kRows = NU * kAppendThreads / kPerRow;
@@ -164,35 +163,44 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const Appe
   const int tid = threadIdx.x;
   uint32_t x = blockIdx.x;
   const int kv = x & 1; x >>= 1;
-  const int h = x % a.Hkv; x /= a.Hkv;
-  const int i = x % a.max_touched, b = x / a.max_touched;
+  int h, b, i = 0;
+  if (kOne) {
+    b = x / a.Hkv; h = x - b * a.Hkv;
+  } else {
+    h = x % a.Hkv; x /= a.Hkv;
+    i = x % a.max_touched; b = x / a.max_touched;
+  }
+  const __nv_bfloat16* rows = (kv ? a.rows[1] : a.rows[0]) + b * a.stride_b + h * a.stride_h;
+  uint4 one = make_uint4(0, 0, 0, 0);
   pdl_wait();
+  if (kOne) one = *reinterpret_cast<const uint4*>(rows + tid % kPerRow * 8);   // (whichever slot it goes to: travels with the count)
   const int64_t n0 = a.n_before[b];
   if (n0 < 0) return;                        // a negative count addresses nothing: the sequence is skipped
   const int64_t n1 = n0 + new_tokens(a.n_new, b, a.T);
-  const TouchedPages t = touched_pages(n0, n1, a.sink, a.window, a.page_tokens);
+  const RingHead head = ring_head(n1, a.sink, a.window);
+  const TouchedPages t = touched_pages(n0, n1, head, a.sink, a.window, a.page_shift);
   if (i >= t.total()) return;
   const int lp = t.page(i);
   const int page = checked_page(a.table[static_cast<int64_t>(b) * a.stride + lp], a.num_pages);
-  if (page < 0) return;
   bool old = false;
   if (tid < kRows) {
-    const int64_t pos = held_position(static_cast<int64_t>(lp) * kRows + tid, n1, a.sink, a.window);
+    const int64_t pos = held_position(lp * kRows + tid, n1, head, a.sink, a.window);
     src[tid] = pos < 0 ? -2 : pos < n0 ? -1 : static_cast<int>(pos - n0);
     old = pos >= 0 && pos < n0;
   }
   const bool any_old = __syncthreads_or(old) != 0;
+  if (page < 0) return;
   const int64_t unit = static_cast<int64_t>(page) * a.Hkv + h;
-  uint8_t* codes = a.pool[kv] + unit * (kRows * D);
-  const float was = any_old ? a.scale[kv][unit] : 0.f;
-  const __nv_bfloat16* rows = a.rows[kv] + b * a.stride_b + h * a.stride_h;
+  uint8_t* codes = (kv ? a.pool[1] : a.pool[0]) + unit * (kRows * D);
+  float* scale = (kv ? a.scale[1] : a.scale[0]) + unit;
+  const float was = any_old ? *scale : 0.f;
   uint4 v[NU];                               // 8 new values, or 8 old codes in (x, y)
-  uint32_t top = 0, top_code = 0;            // largest finite magnitude: bf16 bits, code
+  uint32_t top = 0, top_code = 0;            // largest finite magnitudes: two bf16, a code
 #pragma unroll
   for (int u = 0; u < NU; ++u) {
     const int e = u * kAppendThreads + tid, s = src[e / kPerRow];
     v[u] = make_uint4(0, 0, 0, 0);
-    if (s >= 0) v[u] = *reinterpret_cast<const uint4*>(rows + s * a.stride_t + e % kPerRow * 8);
+    if (s >= 0) v[u] = kOne ? one : *reinterpret_cast<const uint4*>(rows + s * a.stride_t + e % kPerRow * 8);
     else if (s == -1) { const uint2 c = *reinterpret_cast<const uint2*>(codes + e * 8); v[u].x = c.x; v[u].y = c.y; }
   }
 #pragma unroll
@@ -202,9 +210,9 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const Appe
       const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t lo = w[j] & 0x7fffu, hi = (w[j] >> 16) & 0x7fffu;   // infinities and NaN do not count
-        if (lo < 0x7f80u) top = max(top, lo);
-        if (hi < 0x7f80u) top = max(top, hi);
+        uint32_t m = w[j] & 0x7fff7fffu;
+        m &= ~__vcmpgeu2(m, 0x7f807f80u);                                  // infinities and NaN do not count
+        top = __vmaxu2(top, m);
       }
     } else if (s == -1) {
 #pragma unroll
@@ -217,7 +225,7 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const Appe
     }
   }
   const float old_top = f16x2_to_f32x2(e4m3x2_to_f16x2(top_code)).x * was;
-  uint32_t bits = max(top << 16, __float_as_uint(old_top));                // magnitudes: order of the bits
+  uint32_t bits = max(max(top << 16, top & 0xffff0000u), __float_as_uint(old_top));                // magnitudes: order of the bits
   bits = __reduce_max_sync(0xffffffffu, bits);
   if ((tid & 31) == 0) warp_max[tid >> 5] = bits;
   __syncthreads();
@@ -244,7 +252,7 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const Appe
       *reinterpret_cast<uint2*>(codes + e * 8) = out;
     }
   }
-  if (tid == 0) a.scale[kv][unit] = now;
+  if (tid == 0) *scale = now;
 }
 
 // ---- rows of the cache in bf16 ---------------------------------------------------------------
@@ -341,23 +349,27 @@ lg_status launch_paged_linearise(const PagedLinearise& a, int B, cudaStream_t st
 
 // ---- single-token attention ---------------------------------------------------------------------
 // The 32-token tiles of all (sequence, kv head, group of <= 8 query heads) units form one sequence that is cut into equal
-// slices, one per CTA; each of a CTA's warps streams a run of tiles through a ring of its own, filled by TMA from the
-// pages (128-byte or, at D = 64, 64-byte swizzle, so that the fragments are read without bank conflicts).  Scores are
-// S^T = K Q^T and outputs O^T = V^T P^T on mma.sync m16n8k16 with f16 operands: an e4m3 code is an f16 number, so K and V
-// enter without rounding, and q (8 significant bits) does not lose any either once its row is scaled by a power of two.
-// The tensor-core time is far below the HBM's (16 products of 16 x 8 x 16 and 64 conversions per 4 KB of cache, about 80 of
-// 178 cycles of an SM at full bandwidth), a contraction 8 heads wide is far below a tcgen05 tile.
-// A page's scale multiplies its scores; that of V goes into the weights: w_j = 2^(s_j + log2 vs - r) with a running
-// reference r of its own, so that w fits f16 (11 bits) whatever the scales of the pages are, while the row sum is kept in fp32
-// relative to the running maximum m of the scores alone.
-constexpr int kPagedTile = 32;
+// runs, one per warp (a CTA's warps have neighbouring runs).  A warp streams its run through a ring of its own of
+// kPagedSlots half tiles, K and V in turn (cp.async, 16-byte pieces XOR-swizzled by the row, so that fragments are read without
+// bank conflicts); the ring runs on from one unit to the next, so the latencies of a unit (its pages, its scales, its tiles) are
+// paid behind the tiles of the one before.  A unit that lies inside a run is finished by its warp; of the others a warp has
+// at most two pieces, which the CTA merges in shared memory when its runs are done, and units that several CTAs share go through
+// records in the workspace, which the CTA that delivers the last one merges in order.
+// Scores are S^T = K Q^T and outputs O^T = V^T P^T on mma.sync m16n8k16 with f16 operands: an e4m3 code is an f16 number, so K
+// and V enter without rounding, and q (8 significant bits) does not lose any either once its row is scaled by a power of
+// two.  A contraction 8 heads wide is far below a tcgen05 tile.
+// A page's K scale multiplies its scores; that of V goes into the weights: w_j = 2^(s_j + log2 vs - r) with a running reference r of
+// its own, so that w fits f16 (11 bits) whatever the pages' scales are, while the row sum is kept in fp32 relative to the
+// running maximum m of the scores alone.  As long as all pages of a unit have one V scale, r = m + log2 vs and w = p.
+constexpr int kPagedTile = 32, kPagedHalf = 16;   // tokens of a tile, and of what lies in one page whatever its size
+constexpr int kPagedSlots = 5;          // 4 KB each at D = 128: three tiles' K and two tiles' V, or the other way round
 constexpr int kPagedMaxB = 4096;        // sequences of one launch (their prefix sums lie in shared memory)
 constexpr int kPagedMaxCtas = 320;
 
 struct PagedDecodeArgs {
   const __nv_bfloat16* q;        // [B, Hq, D]
-  const float* k_scale;          // [num_pages, Hkv]
-  const float* v_scale;
+  const float* scale[2];         // K, V: [num_pages, Hkv]
+  const uint8_t* pool[2];
   const int32_t* table;          // [B, stride]
   const int64_t* n_tokens;       // [B]
   float* part;
@@ -367,16 +379,19 @@ struct PagedDecodeArgs {
   unsigned int* error_word;
   int B, Hq, Hkv, G, HG, C;
   int sink, block_tokens;
-  int page_shift, num_pages, stride, box_rows;
+  int page_shift, num_pages, stride;
   float scale_log2;
 };
 
-__device__ __forceinline__ void tma_load_2d(uint32_t smem_dst, const void* tmap, uint32_t bar, int c0, int c1) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_dst),
-      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1)
-      : "memory");
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t smem_dst, const void* src) {
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void prefetch_l1(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
 __device__ __forceinline__ void mma16816_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                              uint32_t b1) {
   asm volatile(
@@ -389,298 +404,53 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+__device__ __forceinline__ float fast_log2(float x) {   // (exact for the powers of two of our own scales)
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 template <int D>
 struct PagedSmem {
-  static constexpr int kTileBytes = kPagedTile * D;                     // K (or V) of a tile
-  static constexpr int kPipe = kDecWarps * kDecStages * 2 * kTileBytes;
-  static constexpr int kBars = kPipe;                                   // a barrier per warp and stage
-  static constexpr int kScales = kBars + kDecWarps * kDecStages * 8;    // (k scale, v scale) of a tile's two halves
-  static constexpr int kCum = kScales + kDecWarps * kDecStages * 16;
-  static_assert(kDecWarps * kDecHeads * (D + 2) * 4 <= kPipe, "the merge lies over the rings");
-  static int bytes(int B) { return 1024 /* alignment */ + kCum + (B + 1) * 4; }
+  static constexpr int kSlot = kPagedTile * D;                          // K (or V) of a tile
+  static constexpr int kRing = kPagedSlots * kSlot;                     // of a warp
+  static constexpr int kPiece = kDecHeads * (D + 2) * 4;                // a piece of a unit: O of 8 heads, (m, l) behind each
+  static constexpr int kPieces = kDecWarps * kRing;                     // the piece with which a warp's run begins
+  static constexpr int kScales = kPieces + kDecWarps * kPiece;          // per warp, of three tiles: (K, V) scale of both halves
+  static constexpr int kMeta = kScales + kDecWarps * 3 * 16;            // the units of the warps' pieces: (number, b, k, -), number -1: none
+  static constexpr int kShare = kMeta + kDecWarps * 2 * 16;             // the CTA's first and last unit: (number, first CTA, CTAs, records)
+  static constexpr int kCum = kShare + 2 * 16;
+  static_assert(kPiece <= kRing && kScales % 16 == 0, "the piece with which a run ends lies over the warp's ring");
+  static int bytes(int B) { return kCum + (B + 1) * 4 + B; }
 };
 
-// byte offset of 16-byte chunk c of row r in a tile as TMA lays it out
+// byte offset of 16-byte chunk c of row r in a slot
 template <int D>
 __device__ __forceinline__ uint32_t tile_offset(int r, int c) {
   return r * D + ((c ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4);
 }
 
-// One segment: the CTA's warps stream tiles [tb, te) each of unit (b, kvh, hg) and leave their partial results in shared
-// memory; `it` counts the warp's tiles over all segments.
-template <int D>
-__device__ __forceinline__ bool paged_run_segment(const PagedDecodeArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, uint8_t* sm, int b,
-                                                  int kvh, int hg, int nvalid, int tb, int te, uint32_t& it) {
-  using SM = PagedSmem<D>;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int r = lane >> 2, c = lane & 3;
-  const uint32_t ring = smem_u32(sm) + warp * (kDecStages * 2 * SM::kTileBytes);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(sm + SM::kBars) + warp * kDecStages;
-  float2* scales = reinterpret_cast<float2*>(sm + SM::kScales) + warp * kDecStages * 2;
-  bool ok = true;
-
-  // block-aligned window: the ring's oldest tokens that it leaves out (ex_cnt slots from ring offset ex0 on, cyclic)
-  int ex0 = 0, ex_cnt = 0;
-  const int ring_w = a.C - a.sink;
-  if (a.block_tokens > 0) {
-    const int64_t n = a.n_tokens[b];
-    if (n > a.C) {
-      const int64_t first_held = n - ring_w;
-      const int64_t first_kept = ((n - 1) / a.block_tokens - ring_w / a.block_tokens + 1) * a.block_tokens;
-      if (first_kept > first_held) {
-        ex_cnt = static_cast<int>(first_kept - first_held);
-        ex0 = static_cast<int>((first_held - a.sink) % ring_w);
-      }
-    }
-  }
-  auto attended = [&](int slot) {
-    if (slot >= nvalid) return false;
-    if (ex_cnt == 0 || slot < a.sink) return true;
-    int d = slot - a.sink - ex0;
-    if (d < 0) d += ring_w;
-    return d >= ex_cnt;
-  };
-
-  // q in f16, its row scaled by a power of two to at most 2^11: b0 = dims 16 k + 4 c, +1, b1 = the next two (the pieces of a
-  // row that ldmatrix hands to a thread are four neighbouring bytes, and the order of a product's terms is free)
-  uint32_t qf[D / 16][2];
-  float q_mul;
-  {
-    const int head = hg * kDecHeads + r;
-    const bool on = head < a.G;
-    const uint2* qrow = reinterpret_cast<const uint2*>(a.q + (static_cast<int64_t>(b) * a.Hq + kvh * a.G + (on ? head : 0)) * D);
-    uint2 w[D / 16];
-    uint32_t top = 0;
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-      w[k] = on ? qrow[4 * k + c] : make_uint2(0u, 0u);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t m = ((j & 2 ? w[k].y : w[k].x) >> (16 * (j & 1))) & 0x7fffu;
-        if (m < 0x7f80u) top = max(top, m);
-      }
-    }
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    int e = 137 - static_cast<int>(top >> 7);       // exponent of the factor: the largest value becomes 2^10 to 2^11
-    if (e > 126 || top == 0) e = top == 0 ? 0 : 126;
-    const float mul = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
-    q_mul = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-      qf[k][0] = pack_f16(bf16_lo(w[k].x) * mul, bf16_hi(w[k].x) * mul);
-      qf[k][1] = pack_f16(bf16_lo(w[k].y) * mul, bf16_hi(w[k].y) * mul);
-    }
-  }
-  const float qs0 = __shfl_sync(0xffffffffu, q_mul, 8 * c) * a.scale_log2;
-  const float qs1 = __shfl_sync(0xffffffffu, q_mul, 8 * c + 4) * a.scale_log2;
-
-  float m_run[2] = {-INFINITY, -INFINITY};   // heads 2c, 2c+1: maximum of the scores (log2 domain)
-  float r_run[2] = {-INFINITY, -INFINITY};   // reference of the weights
-  float l_run[2] = {0.f, 0.f};
-  float oacc[D / 16][4];
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) oacc[i][0] = oacc[i][1] = oacc[i][2] = oacc[i][3] = 0.f;
-
-  // pages and scales of the next 32 half tiles to be asked for, one per lane
-  int pg = -1;
-  float ks = 0.f, vs = 0.f;
-  int batch = tb;                            // the tile the batch starts at
-  auto load_batch = [&](int t) {
-    batch = t;
-    const int slot = (2 * t + lane) * (kPagedTile / 2);
-    pg = -1; ks = 0.f; vs = -1.f;            // (a negative scale marks an absent half)
-    if (t + lane / 2 < te && slot < nvalid) {
-      pg = checked_page(a.table[static_cast<int64_t>(b) * a.stride + (slot >> a.page_shift)], a.num_pages);
-      if (pg >= 0) {
-        const int64_t unit = static_cast<int64_t>(pg) * a.Hkv + kvh;
-        ks = a.k_scale[unit];
-        vs = a.v_scale[unit];
-      } else {
-        atomicCAS(a.error_word, 0u, kPageError);
-      }
-    }
-  };
-  uint32_t asked = it;
-  auto issue_tile = [&](int t) {
-    if (t - batch >= 16) load_batch(t);
-    const int x = 2 * (t - batch);
-    const uint32_t stage = asked % kDecStages;
-    const int p0 = __shfl_sync(0xffffffffu, pg, x), p1 = __shfl_sync(0xffffffffu, pg, x + 1);
-    const float k1 = __shfl_sync(0xffffffffu, ks, x + (lane & 1)), v1 = __shfl_sync(0xffffffffu, vs, x + (lane & 1));
-    if (lane < 2) scales[stage * 2 + lane] = make_float2(k1, v1);
-    if (lane == 0) {
-      const int slot = t * kPagedTile, mask = (1 << a.page_shift) - 1;
-      const uint32_t sk = ring + stage * 2 * SM::kTileBytes, sv = sk + SM::kTileBytes, bar = smem_u32(bars + stage);
-      const int r0 = ((p0 * a.Hkv + kvh) << a.page_shift) + (slot & mask);
-      if (a.box_rows == kPagedTile) {
-        mbar_expect_tx(bars + stage, p0 >= 0 ? 2 * SM::kTileBytes : 0);
-        if (p0 >= 0) { tma_load_2d(sk, &tk, bar, 0, r0); tma_load_2d(sv, &tv, bar, 0, r0); }
-      } else {
-        const int r1 = ((p1 * a.Hkv + kvh) << a.page_shift) + ((slot + kPagedTile / 2) & mask);
-        mbar_expect_tx(bars + stage, ((p0 >= 0) + (p1 >= 0)) * SM::kTileBytes);
-        if (p0 >= 0) { tma_load_2d(sk, &tk, bar, 0, r0); tma_load_2d(sv, &tv, bar, 0, r0); }
-        if (p1 >= 0) {
-          tma_load_2d(sk + SM::kTileBytes / 2, &tk, bar, 0, r1);
-          tma_load_2d(sv + SM::kTileBytes / 2, &tv, bar, 0, r1);
-        }
-      }
-    }
-    ++asked;
-  };
-
-  load_batch(tb);
-  for (int t = tb; t < min(te, tb + kDecStages - 1); ++t) issue_tile(t);
-  __syncwarp();                          // the scales of the first tiles
-
-  for (int t = tb; t < te; ++t) {
-    const uint32_t stage = it % kDecStages;
-    ok = ok && mbar_wait_warp(bars + stage, (it / kDecStages) & 1, a.error_word, 20);
-    ++it;
-    if (!ok) break;
-    const uint32_t sk = ring + stage * 2 * SM::kTileBytes, sv = sk + SM::kTileBytes;
-    const float2 sc0 = scales[stage * 2], sc1 = scales[stage * 2 + 1];
-    const bool in0 = sc0.y >= 0.f, in1 = sc1.y >= 0.f;
-
-    // rows that are not attended hold anything at all: a weight of zero does not silence a NaN of V, so those rows are zeroed
-    const int slot0 = t * kPagedTile;
-    const bool edge = slot0 + kPagedTile > nvalid || ex_cnt > 0 || !in0 || !in1;
-    if (edge) {
-      const bool on = attended(slot0 + lane) && (lane < kPagedTile / 2 ? in0 : in1);
-      if (!on) {
-#pragma unroll
-        for (int x = 0; x < D / 16; ++x)
-          asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sv + lane * D + x * 16), "r"(0) : "memory");
-      }
-      __syncwarp();
-    }
-
-    // ---- S^T[32 tokens, 8 heads] = K Q^T
-    float s[2][4] = {};
-    const int row = ((lane >> 3) & 1) * 8 + (lane & 7);
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-#pragma unroll
-      for (int k = 0; k < D / 16; k += 2) {
-        uint32_t x0, x1, x2, x3;              // rows 0-7 and 8-15 of chunk k, the same of chunk k + 1
-        ldsm_x4(sk + tile_offset<D>(16 * x + row, k + (lane >> 4)), x0, x1, x2, x3);
-        mma16816_f16(s[x], e4m3x2_to_f16x2(x0), e4m3x2_to_f16x2(x1), e4m3x2_hi_to_f16x2(x0), e4m3x2_hi_to_f16x2(x1), qf[k][0], qf[k][1]);
-        mma16816_f16(s[x], e4m3x2_to_f16x2(x2), e4m3x2_to_f16x2(x3), e4m3x2_hi_to_f16x2(x2), e4m3x2_hi_to_f16x2(x3), qf[k + 1][0], qf[k + 1][1]);
-      }
-    }
-    // s[x][0, 1]: token 16 x + r, heads 2c, 2c+1; s[x][2, 3]: token 16 x + r + 8.  (Two products: the scales together may leave
-    // the range of fp32 where the score does not.)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const float kk = x ? sc1.x : sc0.x;
-      s[x][0] = s[x][0] * qs0 * kk; s[x][1] = s[x][1] * qs1 * kk;
-      s[x][2] = s[x][2] * qs0 * kk; s[x][3] = s[x][3] * qs1 * kk;
-    }
-    if (edge) {
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const bool in = x ? in1 : in0;
-        if (!in || !attended(slot0 + 16 * x + r)) s[x][0] = s[x][1] = -INFINITY;
-        if (!in || !attended(slot0 + 16 * x + r + 8)) s[x][2] = s[x][3] = -INFINITY;
-      }
-    }
-    // (exact for powers of two; an absent half has no weights)
-    const float lv0 = in0 ? log2f(sc0.y) : in1 ? log2f(sc1.y) : 0.f, lv1 = in1 ? log2f(sc1.y) : lv0;
-    float a0 = fmaxf(s[0][0], s[0][2]), a1 = fmaxf(s[0][1], s[0][3]), b0 = fmaxf(s[1][0], s[1][2]), b1 = fmaxf(s[1][1], s[1][3]);
-    float t0 = fmaxf(a0, b0), t1 = fmaxf(a1, b1);
-#pragma unroll
-    for (int o = 4; o < 32; o <<= 1) {
-      t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, o));
-      t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, o));
-    }
-    float u0 = t0 + lv0, u1 = t1 + lv0;
-    if (lv0 != lv1) {                                                  // the halves lie in pages of different scales
-      u0 = fmaxf(a0 + lv0, b0 + lv1); u1 = fmaxf(a1 + lv0, b1 + lv1);
-#pragma unroll
-      for (int o = 4; o < 32; o <<= 1) {
-        u0 = fmaxf(u0, __shfl_xor_sync(0xffffffffu, u0, o));
-        u1 = fmaxf(u1, __shfl_xor_sync(0xffffffffu, u1, o));
-      }
-    }
-    const float mn0 = fmaxf(m_run[0], t0), mn1 = fmaxf(m_run[1], t1), rn0 = fmaxf(r_run[0], u0), rn1 = fmaxf(r_run[1], u1);
-    const float mu0 = mn0 == -INFINITY ? 0.f : mn0, mu1 = mn1 == -INFINITY ? 0.f : mn1;
-    const float ru0 = rn0 == -INFINITY ? 0.f : rn0, ru1 = rn1 == -INFINITY ? 0.f : rn1;
-    const float al0 = fast_exp2(m_run[0] - mu0), al1 = fast_exp2(m_run[1] - mu1);
-    const float be0 = fast_exp2(r_run[0] - ru0), be1 = fast_exp2(r_run[1] - ru1);
-    m_run[0] = mn0; m_run[1] = mn1; r_run[0] = rn0; r_run[1] = rn1;
-    l_run[0] *= al0; l_run[1] *= al1;
-    uint32_t pb[2][2];                                                 // P^T as the B operand: tokens 2c, +1 of head r, then 8 + 2c, +1
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      l_run[0] += fast_exp2(s[x][0] - mu0) + fast_exp2(s[x][2] - mu0);
-      l_run[1] += fast_exp2(s[x][1] - mu1) + fast_exp2(s[x][3] - mu1);
-      const float lv = x ? lv1 : lv0, d0 = lv - ru0, d1 = lv - ru1;
-      pb[x][0] = movmatrix_t(pack_f16(fast_exp2(s[x][0] + d0), fast_exp2(s[x][1] + d1)));
-      pb[x][1] = movmatrix_t(pack_f16(fast_exp2(s[x][2] + d0), fast_exp2(s[x][3] + d1)));
-    }
-    if (__any_sync(0xffffffffu, be0 != 1.f || be1 != 1.f)) {
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) { oacc[i][0] *= be0; oacc[i][1] *= be1; oacc[i][2] *= be0; oacc[i][3] *= be1; }
-    }
-
-    // ---- O^T[D, 8 heads] += V^T P^T.  Transposed, a thread's 32 bits are dims 2r, 2r+1 of tokens 2c and 2c+1: the even dims are
-    // the product's rows 0-7, the odd ones its rows 8-15.
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-#pragma unroll
-      for (int k = 0; k < D / 16; k += 2) {
-        uint32_t x0, x1, x2, x3;              // tokens 0-7 and 8-15 of chunk k, the same of chunk k + 1
-        ldsm_x4_t(sv + tile_offset<D>(16 * x + row, k + (lane >> 4)), x0, x1, x2, x3);
-        x0 = __byte_perm(x0, 0, 0x3120); x1 = __byte_perm(x1, 0, 0x3120);
-        x2 = __byte_perm(x2, 0, 0x3120); x3 = __byte_perm(x3, 0, 0x3120);
-        mma16816_f16(oacc[k], e4m3x2_to_f16x2(x0), e4m3x2_hi_to_f16x2(x0), e4m3x2_to_f16x2(x1), e4m3x2_hi_to_f16x2(x1), pb[x][0], pb[x][1]);
-        mma16816_f16(oacc[k + 1], e4m3x2_to_f16x2(x2), e4m3x2_hi_to_f16x2(x2), e4m3x2_to_f16x2(x3), e4m3x2_hi_to_f16x2(x3), pb[x][0], pb[x][1]);
-      }
-    }
-    if (edge) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the zeroed rows before the next copy into them
-    __syncwarp();
-    if (t + kDecStages - 1 < te) issue_tile(t + kDecStages - 1);
-  }
-  if (!ok)                                                             // the copies in flight end before the CTA goes on
-    for (; it != asked; ++it) mbar_wait_warp(bars + it % kDecStages, (it / kDecStages) & 1, a.error_word, 21);
-
-  // from the reference of the weights to that of the sums: O relative to m
-#pragma unroll
-  for (int o = 4; o < 32; o <<= 1) {
-    l_run[0] += __shfl_xor_sync(0xffffffffu, l_run[0], o);
-    l_run[1] += __shfl_xor_sync(0xffffffffu, l_run[1], o);
-  }
-  const float g0 = m_run[0] == -INFINITY ? 0.f : fast_exp2(r_run[0] - m_run[0]), g1 = m_run[1] == -INFINITY ? 0.f : fast_exp2(r_run[1] - m_run[1]);
-  __syncthreads();                       // everyone is done with the rings
-  float* mine = reinterpret_cast<float*>(sm) + warp * kDecHeads * (D + 2);
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    *reinterpret_cast<float2*>(mine + (2 * c) * (D + 2) + 16 * i + 2 * r) = make_float2(oacc[i][0] * g0, oacc[i][2] * g0);
-    *reinterpret_cast<float2*>(mine + (2 * c + 1) * (D + 2) + 16 * i + 2 * r) = make_float2(oacc[i][1] * g1, oacc[i][3] * g1);
-  }
-  if (r == 0) {
-    *reinterpret_cast<float2*>(mine + (2 * c) * (D + 2) + D) = make_float2(m_run[0], l_run[0]);
-    *reinterpret_cast<float2*>(mine + (2 * c + 1) * (D + 2) + D) = make_float2(m_run[1], l_run[1]);
-  }
-  __syncthreads();
-  return ok;
-}
-
-// cum[b] = tiles of the sequences before b, b = 0 .. B; returns whether some sequence holds no token.  All threads.
+// tokens that sequence b holds (through the L2: read before and again behind the wait of an overlapped launch)
 __device__ __forceinline__ int paged_valid(const PagedDecodeArgs& a, int b) {
-  const int64_t n = a.n_tokens[b];
+  const int64_t n = __ldcg(reinterpret_cast<const long long*>(a.n_tokens) + b);
   return static_cast<int>(n < a.C ? (n < 0 ? 0 : n) : a.C);
 }
-__device__ __forceinline__ bool paged_build_cum(const PagedDecodeArgs& a, int* cum) {
+
+// cum[b] = tiles of the sequences before b, b = 0 .. B, and behind them a byte per sequence: empty places of its last tile.
+// Returns whether some sequence holds no token; mine: tokens of the thread's first sequence.  All threads.
+__device__ __forceinline__ bool paged_build_cum(const PagedDecodeArgs& a, int* cum, int& mine) {
   __shared__ int warp_sum[kDecWarps];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int each = (a.B + kDecThreads - 1) / kDecThreads, b0 = tid * each, b1 = min(a.B, b0 + each);
   int local = 0;
   bool empty = false;
+  mine = 0;
+#pragma unroll 1
   for (int b = b0; b < b1; ++b) {
-    const int n = (paged_valid(a, b) + kPagedTile - 1) / kPagedTile;
+    const int v = paged_valid(a, b), n = (v + kPagedTile - 1) / kPagedTile;
+    if (b == b0) mine = v;
     cum[b + 1] = n;
+    reinterpret_cast<uint8_t*>(cum + a.B + 1)[b] = static_cast<uint8_t>(n * kPagedTile - v);
     local += n;
     empty |= n == 0;
   }
@@ -692,84 +462,577 @@ __device__ __forceinline__ bool paged_build_cum(const PagedDecodeArgs& a, int* c
   run -= local;
 #pragma unroll
   for (int w = 0; w < kDecWarps; ++w) run += w < warp ? warp_sum[w] : 0;
+#pragma unroll 1
   for (int b = b0; b < b1; ++b) { run += cum[b + 1]; cum[b + 1] = run; }
   if (tid == 0) cum[0] = 0;
   return __syncthreads_or(empty) != 0;
 }
 
+// a place in the sequence of tiles: tile t of the nt of unit (b, kv head, group of query heads)
+struct TilePos {
+  int b, kvh, hg, t, nt;
+  __device__ __forceinline__ void next_unit(const int* cum, int Hkv, int HG) {
+    t = 0;
+    if (++hg < HG) return;
+    hg = 0;
+    if (++kvh < Hkv) return;
+    kvh = 0;
+    do ++b; while (cum[b + 1] == cum[b]);
+    nt = cum[b + 1] - cum[b];
+  }
+};
+
+// The pages of up to 16 tiles of one unit, one half tile per lane.
+constexpr int kNoToken = -2147483647 - 1;   // in place of a table entry: a half tile that holds no token
+struct PageBatch {
+  TilePos at;       // its first tile
+  int count, page;  // tiles; the lane's table entry
+};
+
+// Block-aligned window: the ring's oldest tokens that it leaves out, (first ring offset, number), cyclic.  (Out of line: 64-bit divisions that
+// most calls do not come by.)
+static __device__ __noinline__ int2 left_out(int64_t n, int C, int sink, int block_tokens) {
+  const int w = C - sink;
+  if (n <= C) return make_int2(0, 0);
+  const int64_t first_held = n - w, first_kept = ((n - 1) / block_tokens - w / block_tokens + 1) * block_tokens;
+  if (first_kept <= first_held) return make_int2(0, 0);
+  return make_int2(static_cast<int>((first_held - sink) % w), static_cast<int>(first_kept - first_held));
+}
+
+// Two neighbouring results of a row, and its LSE.
+__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + fast_log2(l)) * 0.6931471805599453f : -INFINITY; }
+
+// The records of a unit, one per CTA from first_cta on, merged in that order into o and lse: a warp per head, a lane per record's weight.
+// The records sit in the L2: their values travel in batches of eight, the first together with the weights.
 template <int D>
-__global__ void __launch_bounds__(kDecThreads) paged_decode_kernel(const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
-                                                                   const PagedDecodeArgs a) {
-  extern __shared__ uint8_t dyn[];
-  using SM = PagedSmem<D>;
-  uint8_t* sm = dyn + ((1024u - (smem_u32(dyn) & 1023u)) & 1023u);      // (the swizzles repeat every 1024 or 512 bytes)
-  int* cum = reinterpret_cast<int*>(sm + SM::kCum);
-  pdl_trigger();
-  if (threadIdx.x < kDecWarps * kDecStages) mbar_init(reinterpret_cast<uint64_t*>(sm + SM::kBars) + threadIdx.x, 1);
-  if (threadIdx.x == 0) { mbar_fence_init(); tma_prefetch_desc(&tk); tma_prefetch_desc(&tv); }
-  pdl_wait();
-  const bool any_empty = paged_build_cum(a, cum);                       // (its barriers order the mbarriers' initialisation too)
-  const int ups = a.Hkv * a.HG, n_cta = gridDim.x, me = blockIdx.x, warp = threadIdx.x >> 5;
-  const int64_t total = static_cast<int64_t>(cum[a.B]) * ups;
-  const bool narrow = total * n_cta <= 0xffffffffll;                    // 64-bit divisions take 200 cycles each
-  auto start_of = [&](int64_t x) -> int64_t {
-    return narrow ? static_cast<uint32_t>(total) * static_cast<uint32_t>(x) / static_cast<uint32_t>(n_cta) : total * x / n_cta;
+__device__ __forceinline__ void merge_records(const PagedDecodeArgs& a, const TilePos& p, int u, int first_cta, int n_rec) {
+  constexpr int V = D / 32;                  // values of a lane
+  const int lane = threadIdx.x & 31, head = threadIdx.x >> 5, gh = p.hg * kDecHeads + head;
+  if (gh >= a.G) return;
+  const float* recs = a.part + (static_cast<int64_t>(first_cta) + u) * (kDecHeads * (D + 2));
+  const float* mine = recs + head * D + lane * V;
+  auto pair = [&](int i) {
+    return i < n_rec ? __ldcg(reinterpret_cast<const float2*>(recs + static_cast<int64_t>(i) * (kDecHeads * (D + 2)) + kDecHeads * D) + head)
+                     : make_float2(-INFINITY, 0.f);
   };
-  auto cta_of = [&](int64_t f) {
-    int64_t x = narrow ? static_cast<uint32_t>(f) * static_cast<uint32_t>(n_cta) / static_cast<uint32_t>(total) : f * n_cta / total;
-    while (x + 1 < n_cta && start_of(x + 1) <= f) ++x;
-    while (x > 0 && start_of(x) > f) --x;
-    return static_cast<int>(x);
-  };
-  const int64_t f0 = start_of(me), f1 = start_of(me + 1);
-  for (int e = 0; any_empty && e < a.B; ++e) {                          // sequences without tokens: their empty results
-    if (cum[e + 1] != cum[e]) continue;
-    for (int x = 0; x < ups; ++x) {
-      const int64_t u = static_cast<int64_t>(e) * ups + x;
-      if (u % n_cta == me) decode_merge_unit<D>(a, reinterpret_cast<float*>(sm), e, x, u, 0, 0, total, n_cta);
+  float m = -INFINITY, l = 0.f, acc[V] = {};
+#pragma unroll 1
+  for (int i = lane; i < n_rec + lane; i += 32) m = fmaxf(m, pair(i).x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll 1
+  for (int i0 = 0; i0 < n_rec; i0 += 32) {
+    const float2 ml = pair(i0 + lane);
+    const float f = fast_exp2(ml.x - mu);
+    l += f * ml.y;
+#pragma unroll 1
+    for (int i = i0; i < min(n_rec, i0 + 32); i += 8) {
+      float v[8][V];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const float* src = mine + static_cast<int64_t>(min(i + x, n_rec - 1)) * (kDecHeads * (D + 2));
+        if (V == 4) {
+          const float4 t = __ldcg(reinterpret_cast<const float4*>(src));
+          v[x][0] = t.x; v[x][1] = t.y; v[x][V - 2] = t.z; v[x][V - 1] = t.w;
+        } else {
+          const float2 t = __ldcg(reinterpret_cast<const float2*>(src));
+          v[x][0] = t.x; v[x][1] = t.y;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const float fx = __shfl_sync(0xffffffffu, f, (i + x) & 31);
+        if (i + x >= n_rec) continue;
+#pragma unroll
+        for (int z = 0; z < V; ++z) acc[z] += fx * v[x][z];
+      }
     }
   }
-  __shared__ int s_last;
-  uint32_t it = 0;
-  int b = 0;
-  if (f0 < f1) {
-    int lo = 0, hi = a.B;                                               // cum[lo] * ups <= f0 < cum[hi] * ups
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  const int64_t qh = static_cast<int64_t>(p.b) * a.Hq + p.kvh * a.G + gh;
+  const float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
+#pragma unroll
+  for (int z = 0; z < V; z += 2)
+    reinterpret_cast<uint32_t*>(a.o + qh * D + lane * V)[z / 2] = l > 0.f ? pack_bf16(acc[z] * inv, acc[z + 1] * inv) : 0u;
+  if (lane == 0 && a.lse) a.lse[qh] = lse_of(m, l);
+}
+
+// (The size of this kernel's code is a time of its own: what a small decode runs once it also fetches once, about 130 cycles for 8
+// instructions.  Hence single copies of what several places need, 32-bit arithmetic, one reciprocal a row.)
+template <int D>
+__global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_kernel(const PagedDecodeArgs a) {
+  extern __shared__ __align__(128) uint8_t sm[];
+  using SM = PagedSmem<D>;
+  int* cum = reinterpret_cast<int*>(sm + SM::kCum);
+  int4* meta = reinterpret_cast<int4*>(sm + SM::kMeta);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+  const int ups = a.Hkv * a.HG, me = blockIdx.x;
+  pdl_trigger();
+
+  uint32_t per = 1, f0 = 0, f1 = 0, g0 = 0, g1 = 0;                     // tiles: of a CTA, my CTA's, my warp's (the host sees to it that all fit 31 bits)
+  auto valid_of = [&](const TilePos& p) { return p.nt * kPagedTile - reinterpret_cast<const uint8_t*>(cum + a.B + 1)[p.b]; };
+  auto find = [&](uint32_t g) {                                         // the place of tile g
+    int lo = 0, hi = a.B;                                               // cum[lo] * ups <= g < cum[hi] * ups
+#pragma unroll 1
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (static_cast<int64_t>(cum[mid]) * ups <= f0) lo = mid; else hi = mid;
+      if (static_cast<uint32_t>(cum[mid]) * ups <= g) lo = mid; else hi = mid;
     }
-    b = lo;
+    TilePos p;
+    p.b = lo;
+    p.nt = cum[lo + 1] - cum[lo];
+    const uint32_t rel = g - static_cast<uint32_t>(cum[lo]) * ups, k = rel / static_cast<uint32_t>(p.nt);
+    p.t = static_cast<int>(rel - k * p.nt);
+    p.kvh = a.HG == 1 ? static_cast<int>(k) : static_cast<int>(k / static_cast<uint32_t>(a.HG));
+    p.hg = static_cast<int>(k) - p.kvh * a.HG;
+    return p;
+  };
+  auto fetch = [&](PageBatch& p, uint32_t left) {                       // count and page of a batch whose place is known
+    p.count = static_cast<int>(min(static_cast<uint32_t>(min(16, p.at.nt - p.at.t)), left));
+    const int slot = p.at.t * kPagedTile + lane * kPagedHalf;           // (the last half tile may hold no token)
+    p.page = lane < 2 * p.count && slot < valid_of(p.at) ? __ldcg(a.table + static_cast<int64_t>(p.at.b) * a.stride + (slot >> a.page_shift)) : kNoToken;
+  };
+  const int in_page = (1 << a.page_shift) - 1;
+  auto row_of = [&](const PageBatch& p, int page) {                     // of the pool: the lane's half tile in that page
+    return ((page * a.Hkv + p.at.kvh) << a.page_shift) + (p.at.t * kPagedTile + lane * kPagedHalf & in_page);
+  };
+  PageBatch next{};                                                     // what is asked for next
+  // the thread's pieces of q: dims 16 k + 4 c to + 3 of head r of the unit's group
+  uint2 qw[D / 16];
+  auto load_q = [&](const TilePos& p) {
+    const int head = p.hg * kDecHeads + r;
+    const uint2* qrow = reinterpret_cast<const uint2*>(a.q + (static_cast<int64_t>(p.b) * a.Hq + p.kvh * a.G + min(head, a.G - 1)) * D) + c;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) qw[k] = qrow[4 * k];
+  };
+
+  // Before the wait: the plan from the counts and the table as they stand, and my first tiles asked into the L2, while the kernel before
+  // (an append) still runs.  What is read here is used for addresses inside the pools only; behind the wait counts and table
+  // are read again, in one trip with q, and the plan is made anew where a count has changed.
+  bool any_empty = false;
+#pragma unroll 1
+  for (int round = a.B <= kDecThreads ? 0 : 1; round < 2; ++round) {
+    int mine = 0;
+    if (round == 1) pdl_wait();
+    any_empty = paged_build_cum(a, cum, mine);
+    const uint32_t total = static_cast<uint32_t>(cum[a.B]) * ups;
+    per = max(1u, (total + gridDim.x - 1) / gridDim.x);
+    f0 = min(total, per * me);
+    f1 = min(total, f0 + per);
+    g0 = f0 + (f1 - f0) * warp / kDecWarps;
+    g1 = f0 + (f1 - f0) * (warp + 1) / kDecWarps;
+    if (g0 < g1) { next.at = find(g0); fetch(next, g1 - g0); }
+    if (warp < 2 && f0 < f1) {                                          // who shares my CTA's first (warp 0) and last unit
+      const TilePos p = find(warp ? f1 - 1 : f0);
+      const uint32_t k = p.kvh * a.HG + p.hg, first = static_cast<uint32_t>(cum[p.b]) * ups + k * p.nt;
+      const int c_lo = static_cast<int>(first / per), c_hi = static_cast<int>((first + p.nt - 1) / per);
+      if (lane == 0) reinterpret_cast<int4*>(sm + SM::kShare)[warp] = make_int4(p.b * ups + k, c_lo, c_hi - c_lo + 1, 0);
+    }
+    if (round == 0) {
+      const int page = checked_page(next.page, a.num_pages);
+      if (g0 < g1 && lane < 2 * min(next.count, 3) && page >= 0) {
+        const int64_t row = row_of(next, page);
+        prefetch_l2(a.pool[0] + row * D, kPagedHalf * D);
+        prefetch_l2(a.pool[1] + row * D, kPagedHalf * D);
+      }
+      pdl_wait();
+      if (g0 < g1) fetch(next, g1 - g0);
+    }
+    if (g0 < g1) load_q(next.at);
+    if (!__syncthreads_or(round == 0 && threadIdx.x < a.B && paged_valid(a, threadIdx.x) != mine)) break;
   }
-  for (int64_t pos = f0; pos < f1;) {
-    while (static_cast<int64_t>(cum[b + 1]) * ups <= pos) ++b;
-    const int nt = cum[b + 1] - cum[b];
-    const int64_t before = static_cast<int64_t>(cum[b]) * ups, rel = pos - before;
-    const int k = narrow ? static_cast<int>(static_cast<uint32_t>(rel) / static_cast<uint32_t>(nt)) : static_cast<int>(rel / nt);
-    const int t0 = static_cast<int>(rel - static_cast<int64_t>(k) * nt);
-    const int n = static_cast<int>(min(static_cast<int64_t>(nt - t0), f1 - pos));
-    const int64_t first = before + static_cast<int64_t>(k) * nt, u = static_cast<int64_t>(b) * ups + k;
-    const int tb = t0 + static_cast<int>(static_cast<int64_t>(n) * warp / kDecWarps);
-    const int te = t0 + static_cast<int>(static_cast<int64_t>(n) * (warp + 1) / kDecWarps);
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");        // what was written over the rings, before the copies into them
-    __syncthreads();
-    const bool direct = t0 == 0 && n == nt;
-    paged_run_segment<D>(a, tk, tv, sm, b, k / a.HG, k % a.HG, paged_valid(a, b), tb, te, it);
-    decode_merge_warps<D>(a, reinterpret_cast<float*>(sm), b, k / a.HG, k % a.HG, a.part + (me + u) * (kDecHeads * (D + 2)), direct);
-    pos += n;
-    if (direct) continue;
-    // the CTA that delivers a unit's last record merges them, in index order, and re-arms the counter
-    const int c_lo = t0 == 0 ? me : cta_of(first), c_hi = t0 + n == nt ? me : cta_of(first + nt - 1);
-    int pieces = c_hi - c_lo + 1;
-    if (total < n_cta)
-      for (int x = c_lo; x <= c_hi; ++x) pieces -= start_of(x) == start_of(x + 1) ? 1 : 0;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      const bool last = ticket_add(a.unit_count + u) + 1u == static_cast<unsigned>(pieces);
-      s_last = last;
-      if (last) a.unit_count[u] = 0u;
+  if (any_empty) {                                                      // sequences without tokens: their empty results
+#pragma unroll 1
+    for (int b = me; b < a.B; b += gridDim.x) {
+      if (cum[b + 1] != cum[b]) continue;
+#pragma unroll 1
+      for (int x = threadIdx.x; x < a.Hq * (D / 2); x += kDecThreads) {
+        reinterpret_cast<uint32_t*>(a.o + static_cast<int64_t>(b) * a.Hq * D)[x] = 0u;
+        if (a.lse && x < a.Hq) a.lse[static_cast<int64_t>(b) * a.Hq + x] = -INFINITY;
+      }
     }
-    __syncthreads();
-    if (s_last) decode_merge_unit<D>(a, reinterpret_cast<float*>(sm), b, k, u, c_lo, c_hi - c_lo + 1, total, n_cta);
+  }
+  if (f0 >= f1) return;
+
+  // ---- my run
+  const uint32_t ring = smem_u32(sm) + warp * SM::kRing, scale_ring = smem_u32(sm + SM::kScales) + warp * 48;
+  TilePos cur = next.at;                                                // what is being worked
+  PageBatch ask = next;                                                 // what is being asked for (empty so far); `next` comes behind it
+  ask.count = 0;
+  uint32_t behind = g0;                                                 // first tile behind `ask`
+  // a copy instruction of the warp brings 512 bytes, 4 rows at D = 128 (whose swizzle alternates from one instruction to the next),
+  // 8 rows at D = 64
+  const uint32_t lane_at = D == 128 ? (lane >> 3) * 128 + (((lane & 7) ^ (lane >> 3)) << 4) : (lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4);
+  int row = -1;                                                         // of the pool, of the lane's half tile in `ask`; -1: nothing there
+  int asked = 0, row0 = -1, row1 = -1, ask_slot = 0, ask_scale = 0;     // tiles of `ask` asked for; the last one's rows
+  auto ask_k = [&]() {                                                  // the next tile's pages and scales
+    if (asked == ask.count) {
+      const bool first = ask.count == 0;
+      ask = next;
+      asked = 0;
+      const int page = checked_page(ask.page, a.num_pages);
+      if (page < 0 && ask.page != kNoToken) atomicCAS(a.error_word, 0u, kPageError);
+      row = page < 0 ? -1 : row_of(ask, page);
+      if (ask.at.t == 0 && !first) {                                    // another unit begins: its q into the L1
+        constexpr int kLines = kDecHeads * D * 2 / 128;
+        if (lane < min(kLines, (a.G - ask.at.hg * kDecHeads) * D * 2 / 128))
+          prefetch_l1(reinterpret_cast<const uint8_t*>(a.q + (static_cast<int64_t>(ask.at.b) * a.Hq + ask.at.kvh * a.G + ask.at.hg * kDecHeads) * D) + lane * 128);
+      }
+      behind += ask.count;
+      if (behind < g1) {
+        next.at.t += ask.count;
+        if (next.at.t == next.at.nt) next.at.next_unit(cum, a.Hkv, a.HG);
+        fetch(next, g1 - behind);
+      }
+    }
+    row0 = __shfl_sync(0xffffffffu, row, 2 * asked);
+    row1 = __shfl_sync(0xffffffffu, row, 2 * asked + 1);
+    ++asked;
+    if (lane < 4) {
+      const int rw = lane < 2 ? row0 : row1;
+      const uint32_t to = scale_ring + ask_scale + lane * 4;
+      if (rw >= 0) copy_async<4>(to, (lane & 1 ? a.scale[1] : a.scale[0]) + (rw >> a.page_shift));
+      else asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(-1.f) : "memory");   // (a negative scale: nothing there)
+    }
+    ask_scale = ask_scale == 32 ? 0 : ask_scale + 16;
+  };
+  auto copy_tile = [&](const uint8_t* pool) {                           // K or V of the tile whose pages were asked for last
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int rw = h ? row1 : row0;
+      if (rw < 0) continue;
+      const uint32_t to = ring + ask_slot + h * (kPagedHalf * D);
+      const uint8_t* from = pool + static_cast<int64_t>(rw) * D + lane * 16;
+#pragma unroll
+      for (int x = 0; x < kPagedHalf * D / 512; ++x)
+        copy_async<16>(D == 128 ? to + x / 2 * 1024 + (x & 1 ? 512 + (lane_at ^ 64) : lane_at) : to + x * 512 + lane_at, from + x * 512);
+    }
+    ask_slot = ask_slot == SM::kRing - SM::kSlot ? 0 : ask_slot + SM::kSlot;
+  };
+
+  uint32_t qf[D / 16][2];
+  float qs0 = 0.f, qs1 = 0.f;                // of heads 2c, 2c+1
+  float m_run[2], r_run[2], l_run[2];        // maximum of the scores (log2 domain), reference of the weights, the thread's share of the sum
+  float oacc[D / 16][4];
+  bool same = true;                          // one V scale so far (vs_ref): r = m + log2 vs_ref
+  float vs_ref = -1.f;
+  int nvalid = 0, ex0 = 0, ex_cnt = 0, first_t = 0;
+  const int ring_w = a.C - a.sink;
+  auto attended = [&](int slot) {
+    if (slot >= nvalid) return false;
+    if (ex_cnt == 0 || slot < a.sink) return true;
+    int d = slot - a.sink - ex0;
+    if (d < 0) d += ring_w;
+    return d >= ex_cnt;
+  };
+  int4 piece[2] = {make_int4(-1, 0, 0, 0), make_int4(-1, 0, 0, 0)};     // the units of my pieces: (number, b, kv head, group)
+  const int n_run = static_cast<int>(g1 - g0);
+  int slot = 0, scale_at = 0;
+  const int frag_row = ((lane >> 3) & 1) * 8 + (lane & 7);
+  auto next_slot = [&]() { slot = slot == SM::kRing - SM::kSlot ? 0 : slot + SM::kSlot; };
+  // (three rounds ahead of the first tile only ask: a second copy of that code in front of the loop would have to be fetched)
+#pragma unroll 1
+  for (int i = -3; i < n_run || i < 0; ++i) {
+    float s[2][4] = {};
+    float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);   // (K, V) scale of the tile's first half, of its second
+    bool in0 = false, in1 = false, edge = false;
+    const int first_slot = cur.t * kPagedTile;
+    if (i >= 0) {
+      if (i == 0 || cur.t == 0) {
+        // A unit begins.  q in f16, its row scaled by a power of two to at most 2^11: b0 = dims 16 k + 4 c, +1, b1 = the next two (the
+        // pieces of a row that ldmatrix hands to a thread are four neighbouring bytes, and the order of a product's terms is free).
+        if (i > 0) load_q(cur);
+        nvalid = valid_of(cur);
+        ex_cnt = 0;
+        if (a.block_tokens > 0) {
+          const int2 x = left_out(a.n_tokens[cur.b], a.C, a.sink, a.block_tokens);
+          ex0 = x.x; ex_cnt = x.y;
+        }
+        uint32_t top = 0;                     // magnitudes of finite values
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            uint32_t w = (j ? qw[k].y : qw[k].x) & 0x7fff7fffu;
+            w &= ~__vcmpgeu2(w, 0x7f807f80u);
+            top = __vmaxu2(top, w);
+          }
+        }
+        top = max(top >> 16, top & 0xffffu);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int e = top == 0 ? 0 : min(126, 137 - static_cast<int>(top >> 7));   // the largest value becomes 2^10 to 2^11
+        const float mul = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+        const float q_mul = __uint_as_float(static_cast<uint32_t>(127 - e) << 23) * a.scale_log2;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          qf[k][0] = pack_f16(bf16_lo(qw[k].x) * mul, bf16_hi(qw[k].x) * mul);
+          qf[k][1] = pack_f16(bf16_lo(qw[k].y) * mul, bf16_hi(qw[k].y) * mul);
+        }
+        qs0 = __shfl_sync(0xffffffffu, q_mul, 8 * c);
+        qs1 = __shfl_sync(0xffffffffu, q_mul, 8 * c + 4);
+        m_run[0] = m_run[1] = r_run[0] = r_run[1] = -INFINITY;
+        l_run[0] = l_run[1] = 0.f;
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x) oacc[x][0] = oacc[x][1] = oacc[x][2] = oacc[x][3] = 0.f;
+        same = true;
+        vs_ref = -1.f;
+        first_t = cur.t;
+      }
+      copy_wait<kPagedSlots - 1>();
+      __syncwarp();                           // K of the tile and its scales are there
+      sc = *reinterpret_cast<const float4*>(sm + SM::kScales + warp * 48 + scale_at);
+      scale_at = scale_at == 32 ? 0 : scale_at + 16;
+      in0 = sc.y >= 0.f; in1 = sc.w >= 0.f;
+      edge = first_slot + kPagedTile > nvalid || !in0 || !in1;
+      if (ex_cnt > 0 && first_slot + kPagedTile > a.sink) {
+        int d = max(first_slot, a.sink) - a.sink - ex0;  // the tile's first ring slot from the first one left out
+        if (d < 0) d += ring_w;
+        edge |= d < ex_cnt || d + kPagedTile > ring_w;
+      }
+
+      // ---- S^T[32 tokens, 8 heads] = K Q^T
+      const uint32_t sk = ring + slot;
+#pragma unroll
+      for (int k = 0; k < D / 16; k += 2) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          uint32_t x0, x1, x2, x3;            // rows 0-7 and 8-15 of chunk k, the same of chunk k + 1
+          ldsm_x4(sk + tile_offset<D>(16 * x + frag_row, k + (lane >> 4)), x0, x1, x2, x3);
+          mma16816_f16(s[x], e4m3x2_to_f16x2(x0), e4m3x2_to_f16x2(x1), e4m3x2_hi_to_f16x2(x0), e4m3x2_hi_to_f16x2(x1), qf[k][0], qf[k][1]);
+          mma16816_f16(s[x], e4m3x2_to_f16x2(x2), e4m3x2_to_f16x2(x3), e4m3x2_hi_to_f16x2(x2), e4m3x2_hi_to_f16x2(x3), qf[k + 1][0], qf[k + 1][1]);
+        }
+      }
+      next_slot();
+      __syncwarp();                           // K has been read
+    }
+    if (i > -3) {
+      if (i + 2 < n_run) copy_tile(a.pool[1]);   // V of the tile whose K was asked for last
+      copy_commit();
+    }
+    if (i >= 0) {
+      // s[x][0, 1]: token 16 x + r, heads 2c, 2c+1; s[x][2, 3]: token 16 x + r + 8.  (The scales together are kept finite: a score of
+      // zero stays zero.)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const float kk = x ? sc.z : sc.x, c0 = fminf(qs0 * kk, 3.4e38f), c1 = fminf(qs1 * kk, 3.4e38f);
+        s[x][0] *= c0; s[x][1] *= c1; s[x][2] *= c0; s[x][3] *= c1;
+      }
+      if (edge) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const bool in = x ? in1 : in0;
+          if (!in || !attended(first_slot + 16 * x + r)) s[x][0] = s[x][1] = -INFINITY;
+          if (!in || !attended(first_slot + 16 * x + r + 8)) s[x][2] = s[x][3] = -INFINITY;
+        }
+      }
+      float t0 = fmaxf(fmaxf(s[0][0], s[0][2]), fmaxf(s[1][0], s[1][2])), t1 = fmaxf(fmaxf(s[0][1], s[0][3]), fmaxf(s[1][1], s[1][3]));
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) {
+        t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, o));
+        t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, o));
+      }
+      const float mn0 = fmaxf(m_run[0], t0), mn1 = fmaxf(m_run[1], t1);
+      const float mu0 = mn0 == -INFINITY ? 0.f : mn0, mu1 = mn1 == -INFINITY ? 0.f : mn1;
+      float be0 = fast_exp2(m_run[0] - mu0), be1 = fast_exp2(m_run[1] - mu1);
+      float w[2][4];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        w[x][0] = fast_exp2(s[x][0] - mu0); w[x][1] = fast_exp2(s[x][1] - mu1);
+        w[x][2] = fast_exp2(s[x][2] - mu0); w[x][3] = fast_exp2(s[x][3] - mu1);
+      }
+      l_run[0] = l_run[0] * be0 + ((w[0][0] + w[0][2]) + (w[1][0] + w[1][2]));
+      l_run[1] = l_run[1] * be1 + ((w[0][1] + w[0][3]) + (w[1][1] + w[1][3]));
+      const float v0 = in0 ? sc.y : in1 ? sc.w : vs_ref, v1 = in1 ? sc.w : v0;   // (a half that is not there has no weights)
+      if (vs_ref < 0.f) vs_ref = v0;
+      if (same && (v0 != vs_ref || v1 != vs_ref)) {   // from here on the weights have a reference of their own
+        same = false;
+        const float lr = fast_log2(vs_ref);
+        r_run[0] = m_run[0] + lr; r_run[1] = m_run[1] + lr;
+      }
+      m_run[0] = mn0; m_run[1] = mn1;
+      if (!same) {
+        const float lv0 = fast_log2(v0), lv1 = fast_log2(v1);
+        float u0 = fmaxf(fmaxf(s[0][0], s[0][2]) + lv0, fmaxf(s[1][0], s[1][2]) + lv1);
+        float u1 = fmaxf(fmaxf(s[0][1], s[0][3]) + lv0, fmaxf(s[1][1], s[1][3]) + lv1);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          u0 = fmaxf(u0, __shfl_xor_sync(0xffffffffu, u0, o));
+          u1 = fmaxf(u1, __shfl_xor_sync(0xffffffffu, u1, o));
+        }
+        const float rn0 = fmaxf(r_run[0], u0), rn1 = fmaxf(r_run[1], u1);
+        const float ru0 = rn0 == -INFINITY ? 0.f : rn0, ru1 = rn1 == -INFINITY ? 0.f : rn1;
+        be0 = fast_exp2(r_run[0] - ru0); be1 = fast_exp2(r_run[1] - ru1);
+        r_run[0] = rn0; r_run[1] = rn1;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const float d0 = (x ? lv1 : lv0) - ru0, d1 = (x ? lv1 : lv0) - ru1;
+          w[x][0] = fast_exp2(s[x][0] + d0); w[x][1] = fast_exp2(s[x][1] + d1);
+          w[x][2] = fast_exp2(s[x][2] + d0); w[x][3] = fast_exp2(s[x][3] + d1);
+        }
+      }
+      if (__any_sync(0xffffffffu, be0 != 1.f || be1 != 1.f)) {
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x) { oacc[x][0] *= be0; oacc[x][1] *= be1; oacc[x][2] *= be0; oacc[x][3] *= be1; }
+      }
+      uint32_t pb[2][2];                      // P^T as the B operand: tokens 2c, +1 of head r, then 8 + 2c, +1
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        pb[x][0] = movmatrix_t(pack_f16(w[x][0], w[x][1]));
+        pb[x][1] = movmatrix_t(pack_f16(w[x][2], w[x][3]));
+      }
+
+      copy_wait<kPagedSlots - 1>();
+      __syncwarp();                           // V of the tile is there
+      const uint32_t sv = ring + slot;
+      if (edge) {   // rows that are not attended hold anything at all: a weight of zero does not silence a NaN of V, so those rows are zeroed
+        if (!((lane < kPagedHalf ? in0 : in1) && attended(first_slot + lane))) {
+#pragma unroll
+          for (int x = 0; x < D / 16; ++x)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sv + lane * D + x * 16), "r"(0) : "memory");
+        }
+        __syncwarp();
+      }
+      // ---- O^T[D, 8 heads] += V^T P^T.  Transposed, a thread's 32 bits are dims 2r, 2r+1 of tokens 2c and 2c+1: the even dims are
+      // the product's rows 0-7, the odd ones its rows 8-15.
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int k = 0; k < D / 16; k += 2) {
+          uint32_t x0, x1, x2, x3;            // tokens 0-7 and 8-15 of chunk k, the same of chunk k + 1
+          ldsm_x4_t(sv + tile_offset<D>(16 * x + frag_row, k + (lane >> 4)), x0, x1, x2, x3);
+          x0 = __byte_perm(x0, 0, 0x3120); x1 = __byte_perm(x1, 0, 0x3120);
+          x2 = __byte_perm(x2, 0, 0x3120); x3 = __byte_perm(x3, 0, 0x3120);
+          mma16816_f16(oacc[k], e4m3x2_to_f16x2(x0), e4m3x2_hi_to_f16x2(x0), e4m3x2_to_f16x2(x1), e4m3x2_hi_to_f16x2(x1), pb[x][0], pb[x][1]);
+          mma16816_f16(oacc[k + 1], e4m3x2_to_f16x2(x2), e4m3x2_hi_to_f16x2(x2), e4m3x2_to_f16x2(x3), e4m3x2_hi_to_f16x2(x3), pb[x][0], pb[x][1]);
+        }
+      }
+      next_slot();
+      __syncwarp();                           // V has been read
+    }
+    if (i + 3 < n_run) { ask_k(); copy_tile(a.pool[0]); }
+    copy_commit();
+    if (i < 0) continue;
+    ++cur.t;
+    const bool tail = cur.t == cur.nt;
+    if (tail || i + 1 == n_run) {
+      // The unit, or my run, ends: the whole unit's result, or a piece (O relative to m).
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) {
+        l_run[0] += __shfl_xor_sync(0xffffffffu, l_run[0], o);
+        l_run[1] += __shfl_xor_sync(0xffffffffu, l_run[1], o);
+      }
+      float g[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) g[x] = m_run[x] == -INFINITY ? 0.f : same ? vs_ref : fast_exp2(r_run[x] - m_run[x]);
+      if (first_t == 0 && tail) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int gh = cur.hg * kDecHeads + 2 * c + x;
+          if (gh >= a.G) continue;
+          const int64_t qh = static_cast<int64_t>(cur.b) * a.Hq + cur.kvh * a.G + gh;
+          const float f = l_run[x] > 0.f ? g[x] * __fdividef(1.f, l_run[x]) : 0.f;
+          uint32_t* to = reinterpret_cast<uint32_t*>(a.o + qh * D) + r;
+#pragma unroll
+          for (int y = 0; y < D / 16; ++y) to[8 * y] = pack_bf16(oacc[y][x] * f, oacc[y][2 + x] * f);
+          if (r == 0 && a.lse) a.lse[qh] = lse_of(m_run[x], l_run[x]);
+        }
+      } else {
+        piece[tail ? 0 : 1] = make_int4(cur.b * ups + cur.kvh * a.HG + cur.hg, cur.b, cur.kvh, cur.hg);
+        float* p = reinterpret_cast<float*>(tail ? sm + SM::kPieces + warp * SM::kPiece : sm + warp * SM::kRing) + (2 * c) * (D + 2);
+#pragma unroll
+        for (int y = 0; y < D / 16; ++y) {
+          *reinterpret_cast<float2*>(p + 16 * y + 2 * r) = make_float2(oacc[y][0] * g[0], oacc[y][2] * g[0]);
+          *reinterpret_cast<float2*>(p + D + 2 + 16 * y + 2 * r) = make_float2(oacc[y][1] * g[1], oacc[y][3] * g[1]);
+        }
+        if (r == 0) {
+          *reinterpret_cast<float2*>(p + D) = make_float2(m_run[0], l_run[0]);
+          *reinterpret_cast<float2*>(p + 2 * D + 2) = make_float2(m_run[1], l_run[1]);
+        }
+      }
+      if (tail && i + 1 < n_run) cur.next_unit(cum, a.Hkv, a.HG);
+    }
+  }
+  if (lane == 0) { meta[2 * warp] = piece[0]; meta[2 * warp + 1] = piece[1]; }
+  __syncthreads();
+
+  // ---- the pieces of my CTA's warps, unit by unit (a warp per head, a lane per piece's weight); what is not a whole unit becomes a record
+  const int4 mine_of = lane < 2 * kDecWarps ? meta[lane] : make_int4(-1, 0, 0, 0);
+  const int4 sh0 = reinterpret_cast<const int4*>(sm + SM::kShare)[0], sh1 = reinterpret_cast<const int4*>(sm + SM::kShare)[1];
+  const float* heads = reinterpret_cast<const float*>(sm) + warp * (D + 2);
+  auto piece_at = [&](int y) { return heads + ((y & 1) ? (y >> 1) * (SM::kRing / 4) : SM::kPieces / 4 + (y >> 1) * (SM::kPiece / 4)); };
+#pragma unroll 1
+  for (unsigned left = __ballot_sync(0xffffffffu, mine_of.x >= 0); left != 0;) {
+    const int y0 = __ffs(left) - 1, u = __shfl_sync(0xffffffffu, mine_of.x, y0);
+    const unsigned mask = __ballot_sync(0xffffffffu, mine_of.x == u);
+    left &= ~mask;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (mask >> lane & 1) ml = *reinterpret_cast<const float2*>(piece_at(lane) + D);
+    float m = ml.x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float f = fast_exp2(ml.x - (m == -INFINITY ? 0.f : m));
+    float l = f * ml.y, acc[D / 32] = {};
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+#pragma unroll 1
+    for (unsigned rest = mask; rest != 0;) {  // two at a time
+      const int y = __ffs(rest) - 1, later = __ffs(rest & (rest - 1)) - 1, z = later < 0 ? y : later;
+      rest &= rest - 1;
+      rest &= rest - 1;
+      const float fy = __shfl_sync(0xffffffffu, f, y), fz = later < 0 ? 0.f : __shfl_sync(0xffffffffu, f, z);
+      const float *p = piece_at(y) + lane * 2, *q = piece_at(z) + lane * 2;
+#pragma unroll
+      for (int x = 0; x < D / 32; x += 2) {
+        const float2 v = *reinterpret_cast<const float2*>(p + 32 * x), w = *reinterpret_cast<const float2*>(q + 32 * x);
+        acc[x] += fy * v.x;
+        acc[x + 1] += fy * v.y;
+        if (later >= 0) { acc[x] += fz * w.x; acc[x + 1] += fz * w.y; }
+      }
+    }
+    if ((u == sh0.x && sh0.z > 1) || (u == sh1.x && sh1.z > 1)) {
+      float* out = a.part + (static_cast<int64_t>(me) + u) * (kDecHeads * (D + 2));
+#pragma unroll
+      for (int x = 0; x < D / 32; x += 2) *reinterpret_cast<float2*>(out + warp * D + lane * 2 + 32 * x) = make_float2(acc[x], acc[x + 1]);
+      if (lane == 0) *reinterpret_cast<float2*>(out + kDecHeads * D + 2 * warp) = make_float2(m, l);
+      continue;
+    }
+    const int b = __shfl_sync(0xffffffffu, mine_of.y, y0), kvh = __shfl_sync(0xffffffffu, mine_of.z, y0);
+    const int gh = __shfl_sync(0xffffffffu, mine_of.w, y0) * kDecHeads + warp;
+    if (gh >= a.G) continue;
+    const int64_t qh = static_cast<int64_t>(b) * a.Hq + kvh * a.G + gh;
+    const float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
+#pragma unroll
+    for (int x = 0; x < D / 32; x += 2)
+      *reinterpret_cast<uint32_t*>(a.o + qh * D + lane * 2 + 32 * x) = l > 0.f ? pack_bf16(acc[x] * inv, acc[x + 1] * inv) : 0u;
+    if (lane == 0 && a.lse) a.lse[qh] = lse_of(m, l);
+  }
+
+  // ---- units that several CTAs share: the one that delivers the last record merges them, in order, and re-arms the counter.  The ticket
+  // releases the CTA's record (its stores are ordered before by the barrier) and acquires the others'.
+  __shared__ int s_last[2];
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    const int4 sh = threadIdx.x ? sh1 : sh0;
+    bool last = false;
+    if (sh.z > 1 && (threadIdx.x == 0 || sh1.x != sh0.x)) {
+      last = ticket_add(a.unit_count + sh.x) + 1u == static_cast<unsigned>(sh.z);
+      if (last) a.unit_count[sh.x] = 0u;
+    }
+    s_last[threadIdx.x] = last;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int x = 0; x < 2; ++x) {
+    if (!s_last[x]) continue;
+    const int4 sh = x ? sh1 : sh0;
+    TilePos p;
+    p.b = sh.x / ups;
+    p.kvh = (sh.x - p.b * ups) / a.HG;
+    p.hg = sh.x - p.b * ups - p.kvh * a.HG;
+    merge_records<D>(a, p, sh.x, sh.y, sh.z);
   }
 }
 
@@ -797,17 +1060,24 @@ lg_status check_paged(const lg_paged_params* p) {
   return LG_OK;
 }
 
+// (A decode's CTA takes nearly all shared memory of an SM, and an SM changes its split of shared memory and L1 only when it is empty: with the
+// same split an overlapped decode gets onto its SM while the append still runs.)
+template <int D, int NU, bool kOne>
+static lg_status launch_append(const AppendArgs& a, unsigned blocks, cudaStream_t stream) {
+  static std::atomic<bool> done[kMaxDevices];
+  auto kern = paged_append_kernel<D, NU, kOne>;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return LG_ERR_CUDA;
+  if (dev >= 0 && dev < kMaxDevices && !done[dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess) cudaGetLastError();
+    done[dev].store(true, std::memory_order_release);
+  }
+  return launch_kernel(true, kern, dim3(blocks), kAppendThreads, 0, stream, a) == cudaSuccess ? LG_OK : LG_ERR_CUDA;
+}
+
 static bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 static bool bad_pools(const void* k_pool, const void* v_pool, const void* k_scale, const void* v_scale) {
   return !k_pool || !v_pool || !k_scale || !v_scale || !aligned16(k_pool) || !aligned16(v_pool) || !aligned(k_scale, 4) || !aligned(v_scale, 4);
-}
-
-// a pool as rows of D bytes, boxes of box_rows rows
-static lg_status pool_tmap(CUtensorMap* out, const void* base, int64_t rows, int D, int box_rows) {
-  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(D)};
-  const cuuint32_t box[2] = {static_cast<cuuint32_t>(D), static_cast<cuuint32_t>(box_rows)};
-  return encode_tmap_u8(out, base, 2, dims, strides, box, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 // The decode kernels may use the dynamic shared memory of their largest batch; said once per device.
@@ -827,23 +1097,24 @@ static lg_status allow_decode_smem() {
 }
 
 struct PagedDecodePlan { int HG, slice, n_cta; int64_t units; size_t count_bytes, total_bytes; };
-static PagedDecodePlan plan_paged_decode(const lg_paged_params* p, int sms) {
+static PagedDecodePlan plan_paged_decode(const lg_paged_params* p) {
   PagedDecodePlan w;
   w.HG = (p->Hq / p->Hkv + kDecHeads - 1) / kDecHeads;
-  w.slice = p->B < kPagedMaxB ? p->B : kPagedMaxB;
-  w.units = static_cast<int64_t>(w.slice) * p->Hkv * w.HG;
+  // sequences of one launch: their prefix sums lie in shared memory, and the kernel counts their tiles in 31 bits
+  const int64_t C = static_cast<int64_t>(p->sink_tokens) + p->window_tokens, seq_units = static_cast<int64_t>(p->Hkv) * w.HG;
+  const int64_t seq_tiles = seq_units * ((C + kPagedTile - 1) / kPagedTile);
+  int64_t most_b = 0x7fffffffll / (seq_tiles + kPagedMaxCtas);
+  if (most_b > kPagedMaxB) most_b = kPagedMaxB;
+  w.slice = static_cast<int>(p->B < most_b ? p->B : most_b);      // (0: one sequence is too long)
+  w.units = w.slice * seq_units;
   w.count_bytes = align_up(static_cast<size_t>(w.units) * sizeof(unsigned int), 256);
   w.total_bytes = sizeof(WsHeader) + w.count_bytes +
                   align_up((static_cast<size_t>(kPagedMaxCtas) + w.units) * kDecHeads * (p->D + 2) * sizeof(float), 256);
-  // a CTA has at least a tile for each two of its warps; as many as fit an SM (D = 64: two), and a whole number of them per unit
-  // where that costs at most a quarter of them (equal lengths then make one segment of every slice)
-  const int64_t C = static_cast<int64_t>(p->sink_tokens) + p->window_tokens;
-  const int64_t tiles = w.units * ((C + kPagedTile - 1) / kPagedTile);
+  // as many CTAs as fit an SM (D = 64: two), each with at least a tile for every second of its warps
+  const int64_t tiles = w.slice * seq_tiles;
   int64_t n = (tiles + kDecWarps / 2 - 1) / (kDecWarps / 2);
-  const int64_t most = (p->D == 64 ? 2 : 1) * static_cast<int64_t>(sms);
+  const int64_t most = (p->D == 64 ? 2 : 1) * kSms;
   if (n > most) n = most;
-  if (n > kPagedMaxCtas) n = kPagedMaxCtas;
-  if (n > w.units && (n / w.units) * w.units * 4 >= n * 3) n = (n / w.units) * w.units;
   w.n_cta = static_cast<int>(n < 1 ? 1 : n);
   return w;
 }
@@ -928,21 +1199,26 @@ lg_status lg_paged_append(const lg_paged_params* p, void* k_pool, void* v_pool, 
   a.rows[0] = static_cast<const __nv_bfloat16*>(k_new); a.rows[1] = static_cast<const __nv_bfloat16*>(v_new);
   a.table = block_table; a.n_before = n_tokens_before; a.n_new = n_new;
   a.B = p->B; a.Hkv = p->Hkv; a.T = T_new; a.sink = p->sink_tokens; a.window = p->window_tokens;
-  a.page_tokens = p->page_tokens; a.num_pages = p->num_pages; a.stride = paged_table_stride(p);
+  a.page_shift = page_shift(p->page_tokens); a.num_pages = p->num_pages; a.stride = paged_table_stride(p);
   a.max_touched = max_touched_pages(T_new, p->sink_tokens, p->window_tokens, p->page_tokens);
   const int64_t blocks = static_cast<int64_t>(p->B) * a.max_touched * p->Hkv * 2;
   if (blocks > 0x7fffffff) return LG_ERR_UNSUPPORTED;
   if ((s = check_arch()) != LG_OK) return s;
   const int nu = p->page_tokens * p->D / 8 / kAppendThreads;
-  auto run = [&](auto kern) {
-    return launch_kernel(true, kern, dim3(static_cast<unsigned>(blocks)), kAppendThreads, 0, static_cast<cudaStream_t>(stream), a) == cudaSuccess
-               ? LG_OK : LG_ERR_CUDA;
-  };
-  if (p->D == 128)
-    return nu == 2 ? run(paged_append_kernel<128, 2>) : nu == 4 ? run(paged_append_kernel<128, 4>)
-         : nu == 8 ? run(paged_append_kernel<128, 8>) : run(paged_append_kernel<128, 16>);
-  return nu == 1 ? run(paged_append_kernel<64, 1>) : nu == 2 ? run(paged_append_kernel<64, 2>)
-       : nu == 4 ? run(paged_append_kernel<64, 4>) : run(paged_append_kernel<64, 8>);
+  const unsigned grid = static_cast<unsigned>(blocks);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+#define LG_APPEND_CASE(DD, NN) \
+  if (p->D == DD && nu == NN) return T_new == 1 ? launch_append<DD, NN, true>(a, grid, st) : launch_append<DD, NN, false>(a, grid, st);
+  LG_APPEND_CASE(128, 2)
+  LG_APPEND_CASE(128, 4)
+  LG_APPEND_CASE(128, 8)
+  LG_APPEND_CASE(128, 16)
+  LG_APPEND_CASE(64, 1)
+  LG_APPEND_CASE(64, 2)
+  LG_APPEND_CASE(64, 4)
+  LG_APPEND_CASE(64, 8)
+#undef LG_APPEND_CASE
+  return LG_ERR_UNSUPPORTED;
 }
 
 lg_status lg_paged_gather(const lg_paged_params* p, const void* k_pool, const void* v_pool, const float* k_scale, const float* v_scale,
@@ -967,7 +1243,9 @@ lg_status lg_paged_gather(const lg_paged_params* p, const void* k_pool, const vo
 }
 
 size_t lg_paged_decode_workspace_bytes(const lg_paged_params* p) {
-  return check_paged(p) == LG_OK ? plan_paged_decode(p, kSms).total_bytes : 0;
+  if (check_paged(p) != LG_OK) return 0;
+  const PagedDecodePlan w = plan_paged_decode(p);
+  return w.slice > 0 ? w.total_bytes : 0;
 }
 
 lg_status lg_paged_decode(const lg_paged_params* p, const void* q, const void* k_pool, const void* v_pool, const float* k_scale,
@@ -979,12 +1257,13 @@ lg_status lg_paged_decode(const lg_paged_params* p, const void* q, const void* k
   if (bad_pools(k_pool, v_pool, k_scale, v_scale) || !q || !block_table || !n_tokens || !o || !workspace) return LG_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(o) || !aligned(block_table, 4) || !aligned(n_tokens, 8) || !aligned(lse, 4) || !aligned(workspace, 256))
     return LG_ERR_INVALID_ARG;
-  const PagedDecodePlan w = plan_paged_decode(p, kSms);
+  const PagedDecodePlan w = plan_paged_decode(p);
+  if (w.slice < 1) return LG_ERR_UNSUPPORTED;
   if (workspace_bytes < w.total_bytes) return LG_ERR_WORKSPACE;
-  if (w.units > 0x7fffffff) return LG_ERR_UNSUPPORTED;
   if ((s = check_arch()) != LG_OK) return s;
   PagedDecodeArgs a;
-  a.k_scale = k_scale; a.v_scale = v_scale;
+  a.scale[0] = k_scale; a.scale[1] = v_scale;
+  a.pool[0] = static_cast<const uint8_t*>(k_pool); a.pool[1] = static_cast<const uint8_t*>(v_pool);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   a.error_word = reinterpret_cast<unsigned int*>(ws);
   a.unit_count = reinterpret_cast<unsigned int*>(ws + sizeof(WsHeader));
@@ -993,24 +1272,19 @@ lg_status lg_paged_decode(const lg_paged_params* p, const void* q, const void* k
   a.C = p->sink_tokens + p->window_tokens;
   a.sink = p->sink_tokens; a.block_tokens = p->block_tokens;
   a.page_shift = page_shift(p->page_tokens); a.num_pages = p->num_pages; a.stride = paged_table_stride(p);
-  a.box_rows = p->page_tokens < kPagedTile ? p->page_tokens : kPagedTile;
   a.scale_log2 = (p->scale > 0.f ? p->scale : 1.0f / sqrtf(static_cast<float>(p->D))) * 1.4426950408889634f;
-  CUtensorMap tk, tv;
-  const int64_t rows = static_cast<int64_t>(p->num_pages) * p->Hkv * p->page_tokens;
-  if ((s = pool_tmap(&tk, k_pool, rows, p->D, a.box_rows)) != LG_OK) return s;
-  if ((s = pool_tmap(&tv, v_pool, rows, p->D, a.box_rows)) != LG_OK) return s;
   if ((s = allow_decode_smem()) != LG_OK) return s;
-  for (int b = 0; b < p->B; b += kPagedMaxB) {   // (larger batches: launch by launch, over the same records)
-    a.B = p->B - b < kPagedMaxB ? p->B - b : kPagedMaxB;
+  for (int b = 0; b < p->B; b += w.slice) {   // (larger batches: launch by launch, over the same records)
+    a.B = p->B - b < w.slice ? p->B - b : w.slice;
     a.q = static_cast<const __nv_bfloat16*>(q) + static_cast<int64_t>(b) * p->Hq * p->D;
     a.o = static_cast<__nv_bfloat16*>(o) + static_cast<int64_t>(b) * p->Hq * p->D;
     a.lse = lse ? lse + static_cast<int64_t>(b) * p->Hq : nullptr;
     a.table = block_table + static_cast<int64_t>(b) * a.stride;
     a.n_tokens = n_tokens + b;
     const cudaError_t e = p->D == 128 ? launch_kernel(true, paged_decode_kernel<128>, dim3(w.n_cta), kDecThreads, PagedSmem<128>::bytes(a.B),
-                                                      static_cast<cudaStream_t>(stream), tk, tv, a)
+                                                      static_cast<cudaStream_t>(stream), a)
                                       : launch_kernel(true, paged_decode_kernel<64>, dim3(w.n_cta), kDecThreads, PagedSmem<64>::bytes(a.B),
-                                                      static_cast<cudaStream_t>(stream), tk, tv, a);
+                                                      static_cast<cudaStream_t>(stream), a);
     if (e != cudaSuccess) return LG_ERR_CUDA;
   }
   return LG_OK;

@@ -16,10 +16,23 @@ __host__ __device__ __forceinline__ int slot_of(int64_t pos, int sink, int windo
   return static_cast<int>(pos < sink ? pos : sink + (pos - sink) % window);
 }
 
-// position of the token that `slot` holds once n tokens have been appended, -1: none yet
-__host__ __device__ __forceinline__ int64_t held_position(int64_t slot, int64_t n, int sink, int window) {
+// Where the newest token of a ring lies: its ring offset, and how often the ring had been filled before its lap (64-bit divisions
+// take 200 cycles: one for all slots of a sequence).  Only meaningful for n > sink.
+struct RingHead {
+  int64_t laps;
+  int offset;
+};
+__host__ __device__ __forceinline__ RingHead ring_head(int64_t n, int sink, int window) {
+  const int64_t d = n - 1 - sink;
+  if (d < window) return RingHead{0, static_cast<int>(d < 0 ? 0 : d)};
+  const int64_t laps = static_cast<uint64_t>(d) <= 0xffffffffull ? static_cast<uint32_t>(d) / static_cast<uint32_t>(window) : d / window;
+  return RingHead{laps, static_cast<int>(d - laps * window)};
+}
+
+// position of the token that `slot` holds once n tokens have been appended, -1: none yet (head: ring_head of n)
+__host__ __device__ __forceinline__ int64_t held_position(int64_t slot, int64_t n, const RingHead& head, int sink, int window) {
   if (slot >= n || slot >= static_cast<int64_t>(sink) + window) return -1;
-  return slot < sink ? slot : slot + (n - 1 - slot) / window * window;
+  return slot < sink ? slot : slot + (slot - sink <= head.offset ? head.laps : head.laps - 1) * window;
 }
 
 // pages that the cache of a sequence of n tokens takes (n < 0 counts as 0)
@@ -36,33 +49,36 @@ struct TouchedPages {
   __host__ __device__ __forceinline__ int total() const { return count[0] + count[1] + count[2]; }
   __host__ __device__ __forceinline__ int page(int i) const {   // 0 <= i < total()
     if (i < count[0]) return first[0] + i;
-    i -= count[0];
-    if (i < count[1]) return first[1] + i;
-    return first[2] + i - count[1];
+    if (i < count[0] + count[1]) return first[1] + i - count[0];
+    return first[2] + i - count[0] - count[1];
   }
 };
-__host__ __device__ __forceinline__ TouchedPages touched_pages(int64_t n0, int64_t n1, int sink, int window, int page_tokens) {
-  int64_t from[3] = {0, 0, 0}, to[3] = {0, 0, 0};              // slot runs [from, to)
-  if (n0 < sink) { from[0] = n0; to[0] = n1 < sink ? n1 : sink; }
+__host__ __device__ __forceinline__ TouchedPages touched_pages(int64_t n0, int64_t n1, const RingHead& head /* of n1 */, int sink, int window,
+                                                               int page_shift) {
+  int from[3] = {0, 0, 0}, to[3] = {0, 0, 0};                  // slot runs [from, to)
+  if (n0 < sink) { from[0] = static_cast<int>(n0); to[0] = n1 < sink ? static_cast<int>(n1) : sink; }
   const int64_t start = n0 > sink ? n0 : sink;                 // first new token of the ring
   if (n1 > start) {
-    const int64_t m = n1 - start < window ? n1 - start : window;   // those of them that survive the call
-    const int64_t r0 = (n1 - m - sink) % window;
-    if (r0 + m <= window) {
-      from[2] = sink + r0; to[2] = sink + r0 + m;
+    const int m = n1 - start < window ? static_cast<int>(n1 - start) : window;   // those of them that survive the call
+    const int r0 = head.offset + 1 - m;                        // ring offset of the oldest of them, below 0: from the lap before
+    if (r0 >= 0) {
+      from[2] = sink + r0; to[2] = sink + head.offset + 1;
     } else {
-      from[2] = sink + r0; to[2] = static_cast<int64_t>(sink) + window;
-      from[1] = sink; to[1] = sink + r0 + m - window;
+      from[2] = sink + r0 + window; to[2] = sink + window;
+      from[1] = sink; to[1] = sink + head.offset + 1;
     }
   }
   TouchedPages t;
-  int64_t next = 0;                                            // first page not listed yet
+  int next = 0;                                                // first page not listed yet
+#ifdef __CUDA_ARCH__
+#pragma unroll
+#endif
   for (int i = 0; i < 3; ++i) {
-    int64_t a = from[i] / page_tokens, b = to[i] > from[i] ? (to[i] - 1) / page_tokens + 1 : a;
+    int a = from[i] >> page_shift, b = to[i] > from[i] ? ((to[i] - 1) >> page_shift) + 1 : a;
     if (a < next) a = next;
     if (b < a) b = a;
-    t.first[i] = static_cast<int>(a);
-    t.count[i] = static_cast<int>(b - a);
+    t.first[i] = a;
+    t.count[i] = b - a;
     if (b > a) next = b;
   }
   return t;

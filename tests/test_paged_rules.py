@@ -23,29 +23,33 @@ using namespace lg;
 int main() {
   std::srand(3);
   for (int i = 0; i < 4000; ++i) {
-    const int sink = std::rand() % 3 == 0 ? 0 : std::rand() % 90, window = 1 + std::rand() % 200, P = 16 << std::rand() % 4;
+    const int sink = std::rand() % 3 == 0 ? 0 : std::rand() % 90, window = 1 + std::rand() % 200, shift = 4 + std::rand() % 4, P = 1 << shift;
     const int64_t n0 = std::rand() % 700, T = std::rand() % 3 == 0 ? 1 : std::rand() % 500, n1 = n0 + T;
     std::map<int, int64_t> held;
     for (int64_t j = 0; j < n1; ++j) held[slot_of(j, sink, window)] = j;
     std::set<int> pages;
+    const RingHead head = ring_head(n1, sink, window);
     for (int s = 0; s < sink + window + 5; ++s) {
       const int64_t want = held.count(s) ? held[s] : -1;
-      if (held_position(s, n1, sink, window) != want) { std::printf("held\n"); return 1; }
+      if (held_position(s, n1, head, sink, window) != want) { std::printf("held\n"); return 1; }
       if (want >= n0) pages.insert(s / P);
     }
-    const TouchedPages t = touched_pages(n0, n1, sink, window, P);
+    const TouchedPages t = touched_pages(n0, n1, head, sink, window, shift);
     if (t.total() != (int)pages.size() || t.total() > max_touched_pages(T, sink, window, P)) { std::printf("count\n"); return 1; }
     int x = 0;
     for (int p : pages) if (t.page(x++) != p) { std::printf("page\n"); return 1; }
     if (pages_of(n1, sink, window, P) != (int)((held.size() + P - 1) / P)) { std::printf("pages_of\n"); return 1; }
   }
-  // far positions: 64-bit counts
-  const int64_t far = (1ll << 40) + 12345;
-  for (int r = 0; r < 300; ++r) {
-    const int s = slot_of(far + r, 7, 300);
-    if (held_position(s, far + 300, 7, 300) != far + r) { std::printf("far\n"); return 1; }
+  // far positions: 64-bit counts, on both sides of 2^32 and far behind
+  for (const int64_t far : {(1ll << 32) - 150, (1ll << 32) + 3, (1ll << 40) + 12345}) {
+    for (int r = 0; r < 300; ++r) {
+      const int s = slot_of(far + r, 7, 300);
+      if (held_position(s, far + 300, ring_head(far + 300, 7, 300), 7, 300) != far + r) { std::printf("far\n"); return 1; }
+    }
+    const TouchedPages t = touched_pages(far, far + 1, ring_head(far + 1, 7, 300), 7, 300, 6);
+    if (t.total() != 1 || t.page(0) != slot_of(far, 7, 300) / 64) { std::printf("far pages\n"); return 1; }
   }
-  if (touched_pages(far, far + 1, 7, 300, 64).total() != 1 || pages_of(-5, 4, 100, 16) != 0) { std::printf("far pages\n"); return 1; }
+  if (pages_of(-5, 4, 100, 16) != 0) { std::printf("negative\n"); return 1; }
   // exponents: the smallest one that covers, over all magnitudes of bf16 and the borders
   for (uint32_t b = 0; b < 0x7f80u; ++b) {
     uint32_t bits = b << 16;
