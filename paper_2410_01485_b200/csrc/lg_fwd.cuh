@@ -55,13 +55,13 @@ struct FwdArgs {
                              // is `phase` tokens into the sequence); win_block = 0: token-exact edge
   const int32_t* doc_start;  // [B, L] first position of each query's document, or null
   float scale_log2;          // scale * log2(e)
+  float max_prob;            // a half's probabilities may grow to this (relative to the row's reference) before the reference moves
   int head_group;            // heads whose CTAs run side by side (cta_coords); >= gridDim.x: all of them
   FwdSplit split;            // tiles cut along their keys
 };
 
 constexpr int kFwdTmaWarp = 8, kFwdMmaWarp0 = 9;
 constexpr int kFwdThreads = 11 * 32;
-constexpr float kFwdMaxProb = 256.0f;   // a half's probabilities may grow to this (relative to the row's reference) before the reference moves
 constexpr int fwd_ctas_per_sm(int bufs) { return bufs == 1 ? 2 : 1; }   // one score buffer per slot: the form of which two share an SM
 template <int D>
 struct FwdSmem {
@@ -438,7 +438,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
         };
         // Probabilities relative to the reference as it stands; the row maximum is only looked at when
         // that cannot be right: the row has no reference yet, or the sum of the half's probabilities
-        // (an upper bound of each of them) passes 2^8.  Otherwise every probability is below 2^8 and the
+        // (an upper bound of each of them) passes max_prob, usually 2^8.  Otherwise every probability is below that and the
         // reference stays -- the maximum, its 32 instructions per row and the vote are off the common path.
         uint32_t preg[32];
         float psum;
@@ -466,7 +466,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
         exp_half(unset ? 0.f : -m_ref);
         // (an unset reference with every column masked gives zeros and stays unset; NaN compares false
         // and cannot appear: masked scores are -inf, whose exponential is 0)
-        const bool look = unset ? (lim > lo) : !(psum <= kFwdMaxProb);
+        const bool look = unset ? (lim > lo) : !(psum <= a.max_prob);
         if (__any_sync(0xffffffffu, look)) {
           float mx = -INFINITY;
 #pragma unroll
