@@ -438,24 +438,30 @@ def paged_params(B, Hq, Hkv, D, sink_tokens, window_tokens, page_tokens, num_pag
     return PagedParams(B, Hq, Hkv, D, sink_tokens, window_tokens, block_tokens, scale, page_tokens, num_pages, table_stride)
 
 
-def _check_cache(p: PagedParams, k_pool, v_pool, k_scale, v_scale, block_table):
-    for pool in (k_pool, v_pool):
-        assert pool.dtype in (torch.float8_e4m3fn, torch.uint8) and pool.is_contiguous()
-        assert tuple(pool.shape) == (p.num_pages, p.Hkv, p.page_tokens, p.D)
-    for s in (k_scale, v_scale):
-        assert s.dtype == torch.float32 and s.is_contiguous() and tuple(s.shape) == (p.num_pages, p.Hkv)
-    if block_table is not None:
-        _check_table(p, block_table)
+_I32, _I64, _F32, _BF16, _F8, _U8 = torch.int32, torch.int64, torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.uint8
+
+
+# (The checks of a call are a microsecond or two of the host's time: every attribute of a tensor is asked for once.)
+def _check_cache(p: PagedParams, k_pool, v_pool, k_scale, v_scale):
+    pages, heads = p.num_pages, p.Hkv
+    pool, scale, code = (pages, heads, p.page_tokens, p.D), (pages, heads), k_pool.dtype
+    assert k_pool.shape == pool and v_pool.shape == pool and k_scale.shape == scale and v_scale.shape == scale, \
+        "expect pools [num_pages, Hkv, page_tokens, D] and scales [num_pages, Hkv]"
+    assert k_pool.is_contiguous() and v_pool.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()
+    assert (code is _F8 or code is _U8) and v_pool.dtype is code and k_scale.dtype is _F32 and v_scale.dtype is _F32
 
 
 def _check_table(p: PagedParams, block_table):
     columns = p.table_stride or -(-(p.sink_tokens + p.window_tokens) // max(1, p.page_tokens))
-    assert block_table.dtype == torch.int32 and block_table.is_contiguous() and tuple(block_table.shape) == (p.B, columns)
+    assert block_table.shape == (p.B, columns) and block_table.dtype is _I32 and block_table.is_contiguous(), \
+        "expect an int32 block table [B, table_stride]"
 
 
-def _check_counts(p: PagedParams, dtype, *counts):
-    for n in counts:
-        assert n is None or (n.dtype == dtype and n.is_contiguous() and n.numel() == p.B)
+def _check_counts(B, dtype, n):
+    assert n.dtype is dtype and n.numel() == B and n.is_contiguous()
+
+
+_Strides = C.c_int64 * 3
 
 
 def _ptr(t):
@@ -466,44 +472,56 @@ def lg_paged_table_extend(p: PagedParams, n_tokens_before, n_new, free_pages, fr
                           T_new: Optional[int] = None):
     """New pages from free_pages (int32) into block_table for sequences that grow from n_tokens_before (int64 [B]) by n_new
     (int32 [B]; None: T_new each) tokens; free_start, free_next: int32 tensors of one element each."""
-    assert n_new is not None or T_new is not None
-    _check_counts(p, torch.int64, n_tokens_before)
-    _check_counts(p, torch.int32, n_new)
+    _check_counts(p.B, _I64, n_tokens_before)
+    if n_new is not None:
+        _check_counts(p.B, _I32, n_new)
+    else:
+        assert T_new is not None
     _check_table(p, block_table)
-    assert free_pages.dtype == free_start.dtype == free_next.dtype == torch.int32 and free_pages.is_contiguous()
-    _check(load_library().lg_paged_table_extend(
+    assert free_pages.dtype is _I32 and free_start.dtype is _I32 and free_next.dtype is _I32 and free_pages.is_contiguous()
+    code = load_library().lg_paged_table_extend(
         C.byref(p), n_tokens_before.data_ptr(), _ptr(n_new), 0x7fffffff if T_new is None else T_new, free_pages.data_ptr(),
-        free_pages.numel(), free_start.data_ptr(), block_table.data_ptr(), free_next.data_ptr(), _stream()),
-        "lg_paged_table_extend")
+        free_pages.numel(), free_start.data_ptr(), block_table.data_ptr(), free_next.data_ptr(), _stream())
+    if code != LG_OK:
+        raise LgError(code, "lg_paged_table_extend")
 
 
 def lg_paged_slot_map(p: PagedParams, n_tokens, first, count, block_table, slot_map):
     """slot_map (int64 [B, T]): where the cache holds positions first .. first + count - 1 (count int32 [B]; None: T)."""
-    _check_counts(p, torch.int64, n_tokens, first)
-    _check_counts(p, torch.int32, count)
+    B, T = slot_map.shape
+    _check_counts(B, _I64, n_tokens)
+    _check_counts(B, _I64, first)
+    if count is not None:
+        _check_counts(B, _I32, count)
     _check_table(p, block_table)
-    assert slot_map.dtype == torch.int64 and slot_map.is_contiguous() and slot_map.shape[0] == p.B
-    _check(load_library().lg_paged_slot_map(C.byref(p), n_tokens.data_ptr(), first.data_ptr(), _ptr(count), slot_map.shape[1],
-                                            block_table.data_ptr(), slot_map.data_ptr(), _stream()), "lg_paged_slot_map")
+    assert B == p.B and slot_map.dtype is _I64 and slot_map.is_contiguous()
+    code = load_library().lg_paged_slot_map(C.byref(p), n_tokens.data_ptr(), first.data_ptr(), _ptr(count), T, block_table.data_ptr(),
+                                            slot_map.data_ptr(), _stream())
+    if code != LG_OK:
+        raise LgError(code, "lg_paged_slot_map")
     return slot_map
 
 
 def _append_args(p: PagedParams, k_pool, v_pool, k_scale, v_scale, block_table, k_new, v_new, n_tokens_before, n_new):
-    _check_cache(p, k_pool, v_pool, k_scale, v_scale, block_table)
-    _check_counts(p, torch.int64, n_tokens_before)
-    _check_counts(p, torch.int32, n_new)
-    shape = tuple(k_new.shape)
-    assert len(shape) == 4 and shape[:2] == (p.B, p.Hkv) and shape[3] == p.D and tuple(v_new.shape) == shape
-    assert k_new.dtype == v_new.dtype == torch.bfloat16
-    whole = (p.Hkv * shape[2] * p.D, shape[2] * p.D, p.D)
-    strides = []
-    for t in (k_new, v_new):   # (the stride of a dimension of one element says nothing)
-        assert t.stride(3) == 1 or shape[2] == 0, "expect contiguous D"
-        strides.append(tuple(w if n == 1 else s for s, n, w in zip(t.stride(), shape, whole)))
-    assert strides[0] == strides[1], "k_new and v_new must have the same strides"
-    st = None if strides[0] == whole else (C.c_int64 * 3)(*strides[0])
+    _check_cache(p, k_pool, v_pool, k_scale, v_scale)
+    _check_table(p, block_table)
+    B, H, T, D = shape = k_new.shape
+    _check_counts(B, _I64, n_tokens_before)
+    if n_new is not None:
+        _check_counts(B, _I32, n_new)
+    assert B == p.B and H == p.Hkv and D == p.D and v_new.shape == shape and k_new.dtype is _BF16 and v_new.dtype is _BF16
+    if k_new.is_contiguous() and v_new.is_contiguous():
+        st = None
+    else:
+        strides, other = k_new.stride(), v_new.stride()
+        if 1 in shape:         # (the stride of a dimension of one element says nothing)
+            whole = (H * T * D, T * D, D, 1)
+            strides, other = (tuple(w if n == 1 else s for s, n, w in zip(x, shape, whole)) for x in (strides, other))
+        assert strides == other, "k_new and v_new must have the same strides"
+        assert strides[3] == 1, "expect contiguous D"
+        st = _Strides(strides[0], strides[1], strides[2])
     return (C.byref(p), k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(),
-            k_new.data_ptr(), v_new.data_ptr(), st, shape[2], n_tokens_before.data_ptr(), _ptr(n_new))
+            k_new.data_ptr(), v_new.data_ptr(), st, T, n_tokens_before.data_ptr(), _ptr(n_new))
 
 
 def lg_paged_append(p: PagedParams, k_pool, v_pool, k_scale, v_scale, block_table, k_new, v_new, n_tokens_before, n_new=None):
@@ -523,15 +541,16 @@ def paged_append_call(p: PagedParams, k_pool, v_pool, k_scale, v_scale, block_ta
 
 def lg_paged_gather(p: PagedParams, k_pool, v_pool, k_scale, v_scale, slot_map, k_out=None, v_out=None):
     """Rows of the cache at slot_map (int64 [B, T]) as bf16 [B, Hkv, T, D]; zeros where it is negative."""
-    _check_cache(p, k_pool, v_pool, k_scale, v_scale, None)
-    assert slot_map.dtype == torch.int64 and slot_map.is_contiguous() and slot_map.shape[0] == p.B
-    T = slot_map.shape[1]
+    _check_cache(p, k_pool, v_pool, k_scale, v_scale)
+    B, T = slot_map.shape
+    assert B == p.B and slot_map.dtype is _I64 and slot_map.is_contiguous()
+    shape = (B, p.Hkv, T, p.D)
     if k_out is None:
-        k_out = torch.empty(p.B, p.Hkv, T, p.D, dtype=torch.bfloat16, device=k_pool.device)
+        k_out = torch.empty(shape, dtype=torch.bfloat16, device=k_pool.device)
     if v_out is None:
         v_out = torch.empty_like(k_out)
     for t in (k_out, v_out):
-        assert t.dtype == torch.bfloat16 and t.is_contiguous() and tuple(t.shape) == (p.B, p.Hkv, T, p.D)
+        assert t.shape == shape and t.dtype is _BF16 and t.is_contiguous()
     _check(load_library().lg_paged_gather(C.byref(p), k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
                                           slot_map.data_ptr(), T, k_out.data_ptr(), v_out.data_ptr(), _stream()), "lg_paged_gather")
     return k_out, v_out
@@ -549,11 +568,13 @@ def paged_decode_workspace(p: PagedParams, device="cuda") -> torch.Tensor:
 
 
 def _decode_args(p: PagedParams, q, k_pool, v_pool, k_scale, v_scale, block_table, n_tokens, o, lse, workspace):
-    _check_cache(p, k_pool, v_pool, k_scale, v_scale, block_table)
-    _check_counts(p, torch.int64, n_tokens)
+    _check_cache(p, k_pool, v_pool, k_scale, v_scale)
+    _check_table(p, block_table)
+    _check_counts(p.B, _I64, n_tokens)
+    shape = (p.B, p.Hq, p.D)
     for t in (q, o):
-        assert t.dtype == torch.bfloat16 and t.is_contiguous() and tuple(t.shape) == (p.B, p.Hq, p.D)
-    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (p.B, p.Hq))
+        assert t.shape == shape and t.dtype is _BF16 and t.is_contiguous()
+    assert lse is None or (lse.shape == shape[:2] and lse.dtype is _F32 and lse.is_contiguous())
     return (C.byref(p), q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
             block_table.data_ptr(), n_tokens.data_ptr(), o.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel())
 
@@ -608,10 +629,11 @@ def lg_paged_chunk_prefill(p: PagedParams, q_chunk, k_chunk, v_chunk, k_pool, v_
                            o=None, lse=None, workspace=None):
     """q_chunk [B,Hq,T,D], k_chunk, v_chunk [B,Hkv,T,D] bf16 against the paged cache; n_tokens_before: B host integers.
     Returns (o [B,Hq,T,D] bf16, lse [B,Hq,T] fp32)."""
-    _check_cache(p, k_pool, v_pool, k_scale, v_scale, block_table)
-    T = q_chunk.shape[2]
+    _check_cache(p, k_pool, v_pool, k_scale, v_scale)
+    _check_table(p, block_table)
+    B, T, D = p.B, q_chunk.shape[2], p.D
     for t, H in ((q_chunk, p.Hq), (k_chunk, p.Hkv), (v_chunk, p.Hkv)):
-        assert t.dtype == torch.bfloat16 and t.is_contiguous() and tuple(t.shape) == (p.B, H, T, p.D)
+        assert t.shape == (B, H, T, D) and t.dtype is _BF16 and t.is_contiguous()
     o = torch.empty_like(q_chunk) if o is None else o
     lse = torch.empty(q_chunk.shape[:3], dtype=torch.float32, device=q_chunk.device) if lse is None else lse
     ws = paged_chunk_prefill_workspace(p, T, n_tokens_before, q_chunk.device) if workspace is None else workspace

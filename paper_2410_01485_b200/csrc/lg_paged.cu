@@ -55,7 +55,7 @@ struct ExtendArgs {
   const int32_t* free_start;
   int32_t* table;
   int32_t* free_next;
-  int B, T_new, n_free, sink, window, page_tokens, stride, rows;
+  int B, T_new, n_free, sink, window, page_shift, stride, rows;
 };
 
 __device__ __forceinline__ int new_tokens(const int32_t* n_new, int b, int T) {
@@ -74,8 +74,8 @@ __global__ void __launch_bounds__(kExtendThreads) table_extend_kernel(const Exte
   pdl_wait();
   auto pages = [&](int b, int& had) {
     const int64_t n = a.n_before[b];
-    had = pages_of(n, a.sink, a.window, a.page_tokens);
-    return n < 0 ? 0 : pages_of(n + new_tokens(a.n_new, b, a.T_new), a.sink, a.window, a.page_tokens);
+    had = pages_of(n, a.sink, a.window, a.page_shift);
+    return n < 0 ? 0 : pages_of(n + new_tokens(a.n_new, b, a.T_new), a.sink, a.window, a.page_shift);
   };
   int64_t sum = 0;
   for (int b = tid; b < b0; b += kExtendThreads) { int h; const int m = pages(b, h); sum += m - h; }
@@ -116,31 +116,46 @@ struct SlotMapArgs {
   int64_t* slot_map;         // [B, T]
   int B, T, sink, window, page_shift, num_pages, stride;
 };
-constexpr int kSlotMapThreads = 256;
+constexpr int kSlotMapThreads = 256, kSlotMapPer = 4;   // tokens of a thread, side by side
 
+// A thread's tokens follow each other in the ring, so one 64-bit division (200 cycles) places all of them; 8 bytes are written a
+// token, and a page's entry comes out of the L1.
 __global__ void __launch_bounds__(kSlotMapThreads) slot_map_kernel(const SlotMapArgs a) {
   pdl_trigger();
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kSlotMapThreads + threadIdx.x;
-  if (i >= static_cast<int64_t>(a.B) * a.T) return;
-  const int b = static_cast<int>(i / a.T), t = static_cast<int>(i - static_cast<int64_t>(b) * a.T);
+  const int b = blockIdx.y, t0 = (blockIdx.x * kSlotMapThreads + threadIdx.x) * kSlotMapPer;
   pdl_wait();
-  const int64_t n = a.n_tokens[b], pos = a.first[b] + t;
-  int64_t out = -1;
-  if (t < new_tokens(a.count, b, a.T) && pos >= 0 && pos < n) {
-    const int slot = slot_of(pos, a.sink, a.window);
-    if (held_position(slot, n, ring_head(n, a.sink, a.window), a.sink, a.window) == pos) {
-      const int page = checked_page(a.table[static_cast<int64_t>(b) * a.stride + (slot >> a.page_shift)], a.num_pages);
-      if (page >= 0) out = (static_cast<int64_t>(page) << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
+  if (t0 >= a.T) return;
+  const int64_t n = a.n_tokens[b], first = a.first[b];
+  const int count = new_tokens(a.count, b, a.T);
+  const int32_t* table = a.table + static_cast<int64_t>(b) * a.stride;
+  // position p of the ring is held iff n - window <= p < n
+  const int64_t p0 = first + t0;
+  int ring = p0 >= a.sink ? slot_of(p0, 0, a.window) - static_cast<int>(a.sink % a.window) : 0;   // ring offset of p0, (p0 - sink) mod window
+  if (ring < 0) ring += a.window;
+  int64_t out[kSlotMapPer];
+#pragma unroll
+  for (int x = 0; x < kSlotMapPer; ++x) {
+    const int64_t p = p0 + x;
+    out[x] = -1;
+    if (t0 + x < count && p >= 0 && p < n && (p < a.sink || p >= n - a.window)) {
+      const int slot = p < a.sink ? static_cast<int>(p) : a.sink + ring;
+      const int page = checked_page(table[slot >> a.page_shift], a.num_pages);
+      if (page >= 0) out[x] = (static_cast<int64_t>(page) << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
     }
+    if (p >= a.sink) ring = ring + 1 == a.window ? 0 : ring + 1;
   }
-  a.slot_map[i] = out;
+  int64_t* to = a.slot_map + static_cast<int64_t>(b) * a.T + t0;
+  if ((reinterpret_cast<uintptr_t>(to) & 15) == 0 && t0 + kSlotMapPer <= a.T) {
+#pragma unroll
+    for (int x = 0; x < kSlotMapPer; x += 2) *reinterpret_cast<longlong2*>(to + x) = make_longlong2(out[x], out[x + 1]);
+  } else {
+#pragma unroll
+    for (int x = 0; x < kSlotMapPer; ++x)
+      if (t0 + x < a.T) to[x] = out[x];
+  }
 }
 
 // ---- append -----------------------------------------------------------------------------------
-// A CTA owns one (sequence, touched page, kv head) of K or of V: it holds the page's new rows (bf16) and its kept old ones
-// (codes) in registers, finds the largest magnitude, and writes codes and scale.  Old rows are written only where the
-// scale changed, and a page whose every live token is new is not read.  HBM-bound for prompts; one round trip for the
-// counts and the table entry, one for the rows and one barrier for a single token.
 struct AppendArgs {
   uint8_t* pool[2];          // K, V: [num_pages, Hkv, P, D]
   float* scale[2];           // [num_pages, Hkv]
@@ -150,30 +165,130 @@ struct AppendArgs {
   const int32_t* n_new;      // or null
   int64_t stride_b, stride_h, stride_t;
   int B, Hkv, T, sink, window, page_shift, num_pages, stride, max_touched;
+  int units, groups;         // many tokens: (K or V, kv head) pairs a CTA works, CTAs per page
 };
-constexpr int kAppendThreads = 128;
 
-template <int D, int NU, bool kOne>   // NU units of 8 elements a thread: page_tokens = NU * 8 * kAppendThreads / D; kOne: one token at most
-__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const AppendArgs a) {
+// Largest finite magnitudes: of two bf16 each (low and high half on their own), of the codes (4 to a word; NaN codes do not count).
+__device__ __forceinline__ uint32_t top_of_new(uint4 v, uint32_t top) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t m = w[j] & 0x7fff7fffu;
+    m &= ~__vcmpgeu2(m, 0x7f807f80u);
+    top = __vmaxu2(top, m);
+  }
+  return top;
+}
+__device__ __forceinline__ uint32_t top_of_old(uint2 v, uint32_t top) {
+  const uint32_t a = v.x & 0x7f7f7f7fu, b = v.y & 0x7f7f7f7fu;
+  return __vmaxu4(top, __vmaxu4(a & ~__vcmpeq4(a, 0x7f7f7f7fu), b & ~__vcmpeq4(b, 0x7f7f7f7fu)));
+}
+// both as the bits of an fp32 magnitude (their order is that of the magnitudes)
+__device__ __forceinline__ uint32_t top_bits(uint32_t top_new, uint32_t top_old, float was) {
+  uint32_t c = __vmaxu4(top_old, top_old >> 16);
+  c = max(c & 0xffu, (c >> 8) & 0xffu);
+  const uint32_t old_bits = __float_as_uint(f16x2_to_f32x2(e4m3x2_to_f16x2(c)).x * was);
+  return max(max(top_new << 16, top_new & 0xffff0000u), c == 0 ? 0u : old_bits);
+}
+__device__ __forceinline__ uint2 code_new(uint4 v, float inv) {
+  return make_uint2(f32x2_to_e4m3x2(bf16_lo(v.x) * inv, bf16_hi(v.x) * inv) | f32x2_to_e4m3x2(bf16_lo(v.y) * inv, bf16_hi(v.y) * inv) << 16,
+                    f32x2_to_e4m3x2(bf16_lo(v.z) * inv, bf16_hi(v.z) * inv) | f32x2_to_e4m3x2(bf16_lo(v.w) * inv, bf16_hi(v.w) * inv) << 16);
+}
+// (two products: was * inv may leave the range of fp32 where every code is zero)
+__device__ __forceinline__ uint32_t recode4(uint32_t c, float was, float inv) {
+  const float2 p = f16x2_to_f32x2(e4m3x2_to_f16x2(c)), q = f16x2_to_f32x2(e4m3x2_hi_to_f16x2(c));
+  return f32x2_to_e4m3x2(p.x * was * inv, p.y * was * inv) | f32x2_to_e4m3x2(q.x * was * inv, q.y * was * inv) << 16;
+}
+__device__ __forceinline__ void scale_of(uint32_t bits, float& now, float& inv) {
+  const int e = page_exponent(bits);
+  now = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+  inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+}
+
+// One token a sequence: a CTA per (sequence, kv head) of K or of V holds the codes of the page that the token goes to (NU units of 8 a
+// thread) and the token's row, finds the largest magnitude and writes the token and, where the scale changed, the others.  What it takes is
+// round trips: count, table entry, codes and scale.  Count and entry are read before the wait of an overlapped launch too, so that
+// behind it all three travel at once; only where one has changed do they follow each other.
+template <int D, int NU>
+__global__ void __launch_bounds__(128) paged_append_one_kernel(const AppendArgs a) {
   pdl_trigger();
-  constexpr int kPerRow = D / 8, kRows = NU * kAppendThreads / kPerRow;
-  static_assert(kRows <= kAppendThreads, "a thread per slot of the page");
+  constexpr int kThreads = 128, kPerRow = D / 8, kRows = NU * kThreads / kPerRow;
+  __shared__ uint32_t warp_max[2][kThreads / 32];
+  const int tid = threadIdx.x;
+  const uint32_t x = blockIdx.x >> 1, kv = blockIdx.x & 1, b = x / static_cast<uint32_t>(a.Hkv), h = x - b * a.Hkv;
+  const int t = a.n_new ? -1 : 1;
+  auto count = [&]() { return __ldcg(reinterpret_cast<const long long*>(a.n_before) + b); };
+  auto entry = [&](int64_t n) { return n < 0 ? -1 : __ldcg(a.table + static_cast<int64_t>(b) * a.stride + (slot_of(n, a.sink, a.window) >> a.page_shift)); };
+  int64_t n0 = count();
+  int lp_entry = entry(n0);
+  pdl_wait();
+#pragma unroll 1
+  for (int round = 0; round < 4; ++round) {   // (the second is the last, unless someone writes the counts meanwhile)
+    const int64_t n_seen = n0;
+    const int entry_seen = lp_entry;
+    n0 = count();
+    lp_entry = entry(n_seen);
+    const bool none = t < 0 && a.n_new[b] < 1;
+    const int slot = n_seen < 0 ? 0 : slot_of(n_seen, a.sink, a.window), page = checked_page(entry_seen, a.num_pages);
+    const int at = slot & (kRows - 1);                                   // the token's row in its page
+    const int64_t after = n_seen + 1, cap = static_cast<int64_t>(a.sink) + a.window;
+    const int held = static_cast<int>((after < cap ? after : cap) - (slot - at));   // slots of the page, from its first one on, that hold a token
+    const int64_t unit = static_cast<int64_t>(page < 0 ? 0 : page) * a.Hkv + h;
+    uint8_t* codes = (kv ? a.pool[1] : a.pool[0]) + unit * (kRows * D);
+    float* scale = (kv ? a.scale[1] : a.scale[0]) + unit;
+    const uint4 row = *reinterpret_cast<const uint4*>((kv ? a.rows[1] : a.rows[0]) + b * a.stride_b + h * a.stride_h + tid % kPerRow * 8);
+    const float was = *scale;
+    uint2 v[NU];
+    uint32_t top = top_of_new(row, 0u), top_old = 0;                     // (every row's threads look at the whole token)
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      const int e = u * kThreads + tid, rr = e / kPerRow;
+      v[u] = rr < held && rr != at ? *reinterpret_cast<const uint2*>(codes + e * 8) : make_uint2(0u, 0u);
+    }
+#pragma unroll
+    for (int u = 0; u < NU; ++u) top_old = top_of_old(v[u], top_old);
+    uint32_t bits = __reduce_max_sync(0xffffffffu, top_bits(top, top_old, was));
+    if (__any_sync(0xffffffffu, n0 != n_seen || lp_entry != entry_seen)) bits = 0xffffffffu;   // the plan was of another time
+    if ((tid & 31) == 0) warp_max[round & 1][tid >> 5] = bits;
+    __syncthreads();
+    bits = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) bits = max(bits, warp_max[round & 1][w]);
+    if (bits == 0xffffffffu) {
+      if (n0 != n_seen) lp_entry = entry(n0);
+      continue;
+    }
+    if (n_seen < 0 || none || page < 0) return;
+    float now, inv;
+    scale_of(bits, now, inv);
+    const bool rescale = held > 1 && was != now;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      const int e = u * kThreads + tid, rr = e / kPerRow;
+      if (rr == at) *reinterpret_cast<uint2*>(codes + e * 8) = code_new(row, inv);
+      else if (rescale && rr < held) *reinterpret_cast<uint2*>(codes + e * 8) = make_uint2(recode4(v[u].x, was, inv), recode4(v[u].y, was, inv));
+    }
+    if (tid == 0) *scale = now;
+    return;
+  }
+}
+
+// Several tokens a sequence: a CTA takes one page that a sequence's tokens go to, for some of the (K or V, kv head) pairs one after
+// the other.  It holds a pair's new rows (bf16) and its kept old ones (codes) in registers, finds the largest magnitude, and writes codes and
+// scale, while the next pair's rows are on their way.  Old rows are written only where the scale changed, and a page whose live tokens are all
+// new is not read.  HBM-bound.
+template <int D, int NU, int kThreads>   // NU units of 8 elements a thread: page_tokens = NU * 8 * kThreads / D
+__global__ void __launch_bounds__(kThreads) paged_append_kernel(const AppendArgs a) {
+  pdl_trigger();
+  constexpr int kPerRow = D / 8, kRows = NU * kThreads / kPerRow;
+  static_assert(kRows <= kThreads, "a thread per slot of the page");
   __shared__ int src[kRows];                 // new token of each slot; -1: kept old one; -2: nothing
-  __shared__ uint32_t warp_max[kAppendThreads / 32];
+  __shared__ uint32_t warp_max[2][kThreads / 32];
   const int tid = threadIdx.x;
   uint32_t x = blockIdx.x;
-  const int kv = x & 1; x >>= 1;
-  int h, b, i = 0;
-  if (kOne) {
-    b = x / a.Hkv; h = x - b * a.Hkv;
-  } else {
-    h = x % a.Hkv; x /= a.Hkv;
-    i = x % a.max_touched; b = x / a.max_touched;
-  }
-  const __nv_bfloat16* rows = (kv ? a.rows[1] : a.rows[0]) + b * a.stride_b + h * a.stride_h;
-  uint4 one = make_uint4(0, 0, 0, 0);
+  const int g = x % a.groups; x /= a.groups;
+  const int i = x % a.max_touched, b = x / a.max_touched;
   pdl_wait();
-  if (kOne) one = *reinterpret_cast<const uint4*>(rows + tid % kPerRow * 8);   // (whichever slot it goes to: travels with the count)
   const int64_t n0 = a.n_before[b];
   if (n0 < 0) return;                        // a negative count addresses nothing: the sequence is skipped
   const int64_t n1 = n0 + new_tokens(a.n_new, b, a.T);
@@ -190,69 +305,59 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(const Appe
   }
   const bool any_old = __syncthreads_or(old) != 0;
   if (page < 0) return;
-  const int64_t unit = static_cast<int64_t>(page) * a.Hkv + h;
-  uint8_t* codes = (kv ? a.pool[1] : a.pool[0]) + unit * (kRows * D);
-  float* scale = (kv ? a.scale[1] : a.scale[0]) + unit;
-  const float was = any_old ? *scale : 0.f;
-  uint4 v[NU];                               // 8 new values, or 8 old codes in (x, y)
-  uint32_t top = 0, top_code = 0;            // largest finite magnitudes: two bf16, a code
+  int from[NU];                              // src of my units
 #pragma unroll
-  for (int u = 0; u < NU; ++u) {
-    const int e = u * kAppendThreads + tid, s = src[e / kPerRow];
-    v[u] = make_uint4(0, 0, 0, 0);
-    if (s >= 0) v[u] = kOne ? one : *reinterpret_cast<const uint4*>(rows + s * a.stride_t + e % kPerRow * 8);
-    else if (s == -1) { const uint2 c = *reinterpret_cast<const uint2*>(codes + e * 8); v[u].x = c.x; v[u].y = c.y; }
-  }
+  for (int u = 0; u < NU; ++u) from[u] = src[(u * kThreads + tid) / kPerRow];
+  const int last = min((g + 1) * a.units, 2 * a.Hkv);
+  uint4 next[NU], v[NU];
+  float was_next = 0.f, was;
+  auto load = [&](int pair) {                // 8 new values a unit, or 8 old codes in (x, y)
+    const int kv = pair >= a.Hkv, h = pair - (kv ? a.Hkv : 0);
+    const int64_t unit = static_cast<int64_t>(page) * a.Hkv + h;
+    const __nv_bfloat16* rows = (kv ? a.rows[1] : a.rows[0]) + b * a.stride_b + h * a.stride_h;
+    const uint8_t* codes = (kv ? a.pool[1] : a.pool[0]) + unit * (kRows * D);
 #pragma unroll
-  for (int u = 0; u < NU; ++u) {
-    const int s = src[(u * kAppendThreads + tid) / kPerRow];
-    if (s >= 0) {
-      const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t m = w[j] & 0x7fff7fffu;
-        m &= ~__vcmpgeu2(m, 0x7f807f80u);                                  // infinities and NaN do not count
-        top = __vmaxu2(top, m);
-      }
-    } else if (s == -1) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        uint32_t c = (j ? v[u].y : v[u].x) & 0x7f7f7f7fu;
-        c &= ~__vcmpeq4(c, 0x7f7f7f7fu);                                   // NaN codes do not count
-        const uint32_t m = __vmaxu4(c, c >> 16);
-        top_code = max(top_code, max(m & 0xffu, (m >> 8) & 0xffu));
-      }
+    for (int u = 0; u < NU; ++u) {
+      const int e = u * kThreads + tid;
+      next[u] = make_uint4(0, 0, 0, 0);
+      if (from[u] >= 0) next[u] = *reinterpret_cast<const uint4*>(rows + from[u] * a.stride_t + e % kPerRow * 8);
+      else if (from[u] == -1) { const uint2 c = *reinterpret_cast<const uint2*>(codes + e * 8); next[u].x = c.x; next[u].y = c.y; }
     }
-  }
-  const float old_top = f16x2_to_f32x2(e4m3x2_to_f16x2(top_code)).x * was;
-  uint32_t bits = max(max(top << 16, top & 0xffff0000u), __float_as_uint(old_top));                // magnitudes: order of the bits
-  bits = __reduce_max_sync(0xffffffffu, bits);
-  if ((tid & 31) == 0) warp_max[tid >> 5] = bits;
-  __syncthreads();
-  bits = 0;
+    if (any_old) was_next = (kv ? a.scale[1] : a.scale[0])[unit];
+  };
+  load(g * a.units);
+#pragma unroll 1
+  for (int pair = g * a.units; pair < last; ++pair) {
 #pragma unroll
-  for (int w = 0; w < kAppendThreads / 32; ++w) bits = max(bits, warp_max[w]);
-  const int e2 = page_exponent(bits);
-  const float now = __uint_as_float(static_cast<uint32_t>(e2 + 127) << 23), inv = __uint_as_float(static_cast<uint32_t>(127 - e2) << 23);
-  const bool rescale = any_old && was != now;
+    for (int u = 0; u < NU; ++u) v[u] = next[u];
+    was = was_next;
+    if (pair + 1 < last) load(pair + 1);
+    uint32_t top = 0, top_old = 0;
 #pragma unroll
-  for (int u = 0; u < NU; ++u) {
-    const int e = u * kAppendThreads + tid, s = src[e / kPerRow];
-    uint2 out;
-    if (s >= 0) {
-      out.x = f32x2_to_e4m3x2(bf16_lo(v[u].x) * inv, bf16_hi(v[u].x) * inv) | f32x2_to_e4m3x2(bf16_lo(v[u].y) * inv, bf16_hi(v[u].y) * inv) << 16;
-      out.y = f32x2_to_e4m3x2(bf16_lo(v[u].z) * inv, bf16_hi(v[u].z) * inv) | f32x2_to_e4m3x2(bf16_lo(v[u].w) * inv, bf16_hi(v[u].w) * inv) << 16;
-      *reinterpret_cast<uint2*>(codes + e * 8) = out;
-    } else if (s == -1 && rescale) {
-      const float2 p = f16x2_to_f32x2(e4m3x2_to_f16x2(v[u].x)), q = f16x2_to_f32x2(e4m3x2_hi_to_f16x2(v[u].x));
-      const float2 r = f16x2_to_f32x2(e4m3x2_to_f16x2(v[u].y)), w = f16x2_to_f32x2(e4m3x2_hi_to_f16x2(v[u].y));
-      // (two products: was * inv may leave the range of fp32 where every code is zero)
-      out.x = f32x2_to_e4m3x2(p.x * was * inv, p.y * was * inv) | f32x2_to_e4m3x2(q.x * was * inv, q.y * was * inv) << 16;
-      out.y = f32x2_to_e4m3x2(r.x * was * inv, r.y * was * inv) | f32x2_to_e4m3x2(w.x * was * inv, w.y * was * inv) << 16;
-      *reinterpret_cast<uint2*>(codes + e * 8) = out;
+    for (int u = 0; u < NU; ++u) {
+      if (from[u] >= 0) top = top_of_new(v[u], top);
+      else if (from[u] == -1) top_old = top_of_old(make_uint2(v[u].x, v[u].y), top_old);
     }
+    uint32_t bits = __reduce_max_sync(0xffffffffu, top_bits(top, top_old, was));
+    if ((tid & 31) == 0) warp_max[pair & 1][tid >> 5] = bits;
+    __syncthreads();
+    bits = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) bits = max(bits, warp_max[pair & 1][w]);
+    float now, inv;
+    scale_of(bits, now, inv);
+    const bool rescale = any_old && was != now;
+    const int kv = pair >= a.Hkv, h = pair - (kv ? a.Hkv : 0);
+    const int64_t unit = static_cast<int64_t>(page) * a.Hkv + h;
+    uint8_t* codes = (kv ? a.pool[1] : a.pool[0]) + unit * (kRows * D);
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      uint2* to = reinterpret_cast<uint2*>(codes + (u * kThreads + tid) * 8);
+      if (from[u] >= 0) *to = code_new(v[u], inv);
+      else if (from[u] == -1 && rescale) *to = make_uint2(recode4(v[u].x, was, inv), recode4(v[u].y, was, inv));
+    }
+    if (tid == 0) (kv ? a.scale[1] : a.scale[0])[unit] = now;
   }
-  if (tid == 0) *scale = now;
 }
 
 // ---- rows of the cache in bf16 ---------------------------------------------------------------
@@ -1062,17 +1167,17 @@ lg_status check_paged(const lg_paged_params* p) {
 
 // (A decode's CTA takes nearly all shared memory of an SM, and an SM changes its split of shared memory and L1 only when it is empty: with the
 // same split an overlapped decode gets onto its SM while the append still runs.)
-template <int D, int NU, bool kOne>
-static lg_status launch_append(const AppendArgs& a, unsigned blocks, cudaStream_t stream) {
+template <int D, int NU>
+static lg_status launch_append_one(const AppendArgs& a, unsigned blocks, cudaStream_t stream) {
   static std::atomic<bool> done[kMaxDevices];
-  auto kern = paged_append_kernel<D, NU, kOne>;
+  auto kern = paged_append_one_kernel<D, NU>;
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess) return LG_ERR_CUDA;
   if (dev >= 0 && dev < kMaxDevices && !done[dev].load(std::memory_order_acquire)) {
     if (cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess) cudaGetLastError();
     done[dev].store(true, std::memory_order_release);
   }
-  return launch_kernel(true, kern, dim3(blocks), kAppendThreads, 0, stream, a) == cudaSuccess ? LG_OK : LG_ERR_CUDA;
+  return launch_kernel(true, kern, dim3(blocks), 128, 0, stream, a) == cudaSuccess ? LG_OK : LG_ERR_CUDA;
 }
 
 static bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -1141,7 +1246,7 @@ lg_status lg_paged_table_extend(const lg_paged_params* p, const int64_t* n_token
   a.n_before = n_tokens_before; a.n_new = n_new; a.free_pages = free_pages; a.free_start = free_start;
   a.table = block_table; a.free_next = free_next;
   a.B = p->B; a.T_new = T_new; a.n_free = n_free;
-  a.sink = p->sink_tokens; a.window = p->window_tokens; a.page_tokens = p->page_tokens; a.stride = paged_table_stride(p);
+  a.sink = p->sink_tokens; a.window = p->window_tokens; a.page_shift = page_shift(p->page_tokens); a.stride = paged_table_stride(p);
   a.rows = (p->B + 2 * kSms - 1) / (2 * kSms);
   if (a.rows > kExtendMaxRows) a.rows = kExtendMaxRows;
   int64_t most = static_cast<int64_t>(T_new) / p->page_tokens + 1;       // new pages of a sequence
@@ -1162,14 +1267,14 @@ lg_status lg_paged_slot_map(const lg_paged_params* p, const int64_t* n_tokens, c
   if (!n_tokens || !first || !block_table || !slot_map) return LG_ERR_INVALID_ARG;
   if (!aligned(n_tokens, 8) || !aligned(first, 8) || !aligned(count, 4) || !aligned(block_table, 4) || !aligned(slot_map, 8))
     return LG_ERR_INVALID_ARG;
-  const int64_t blocks = (static_cast<int64_t>(p->B) * T + kSlotMapThreads - 1) / kSlotMapThreads;
-  if (blocks > 0x7fffffff) return LG_ERR_UNSUPPORTED;
+  const int64_t blocks = (static_cast<int64_t>(T) + kSlotMapThreads * kSlotMapPer - 1) / (kSlotMapThreads * kSlotMapPer);
+  if (p->B > 65535 || T > (1 << 30)) return LG_ERR_UNSUPPORTED;
   if ((s = check_arch()) != LG_OK) return s;
   SlotMapArgs a;
   a.n_tokens = n_tokens; a.first = first; a.count = count; a.table = block_table; a.slot_map = slot_map;
   a.B = p->B; a.T = T; a.sink = p->sink_tokens; a.window = p->window_tokens;
   a.page_shift = page_shift(p->page_tokens); a.num_pages = p->num_pages; a.stride = paged_table_stride(p);
-  return launch_kernel(true, slot_map_kernel, dim3(static_cast<unsigned>(blocks)), kSlotMapThreads, 0, static_cast<cudaStream_t>(stream), a) ==
+  return launch_kernel(true, slot_map_kernel, dim3(static_cast<unsigned>(blocks), p->B), kSlotMapThreads, 0, static_cast<cudaStream_t>(stream), a) ==
                  cudaSuccess ? LG_OK : LG_ERR_CUDA;
 }
 
@@ -1201,22 +1306,32 @@ lg_status lg_paged_append(const lg_paged_params* p, void* k_pool, void* v_pool, 
   a.B = p->B; a.Hkv = p->Hkv; a.T = T_new; a.sink = p->sink_tokens; a.window = p->window_tokens;
   a.page_shift = page_shift(p->page_tokens); a.num_pages = p->num_pages; a.stride = paged_table_stride(p);
   a.max_touched = max_touched_pages(T_new, p->sink_tokens, p->window_tokens, p->page_tokens);
-  const int64_t blocks = static_cast<int64_t>(p->B) * a.max_touched * p->Hkv * 2;
+  // one token: a CTA per (K or V, kv head).  Several: as many of them one after the other as leave eight CTAs an SM (a CTA's counts and table
+  // entry are two round trips that the next pair's rows do not wait for)
+  const int64_t pages = static_cast<int64_t>(p->B) * a.max_touched, pairs = 2ll * p->Hkv;
+  int64_t units = T_new == 1 ? 1 : pages * pairs / (8 * kSms);
+  units = units < 1 ? 1 : units > pairs ? pairs : units;
+  a.units = static_cast<int>(units);
+  a.groups = static_cast<int>((pairs + units - 1) / units);
+  const int64_t blocks = pages * a.groups;
   if (blocks > 0x7fffffff) return LG_ERR_UNSUPPORTED;
   if ((s = check_arch()) != LG_OK) return s;
-  const int nu = p->page_tokens * p->D / 8 / kAppendThreads;
   const unsigned grid = static_cast<unsigned>(blocks);
+  const int elements = p->page_tokens * p->D;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-#define LG_APPEND_CASE(DD, NN) \
-  if (p->D == DD && nu == NN) return T_new == 1 ? launch_append<DD, NN, true>(a, grid, st) : launch_append<DD, NN, false>(a, grid, st);
-  LG_APPEND_CASE(128, 2)
-  LG_APPEND_CASE(128, 4)
-  LG_APPEND_CASE(128, 8)
-  LG_APPEND_CASE(128, 16)
-  LG_APPEND_CASE(64, 1)
-  LG_APPEND_CASE(64, 2)
-  LG_APPEND_CASE(64, 4)
-  LG_APPEND_CASE(64, 8)
+#define LG_APPEND_CASE(DD, PP, TT)                                                                \
+  if (p->D == DD && elements == DD * PP) {                                                        \
+    if (T_new == 1) return launch_append_one<DD, DD * PP / 1024>(a, grid, st);                    \
+    return launch_kernel(true, paged_append_kernel<DD, DD * PP / 8 / TT, TT>, dim3(grid), TT, 0, st, a) == cudaSuccess ? LG_OK : LG_ERR_CUDA; \
+  }
+  LG_APPEND_CASE(128, 16, 128)
+  LG_APPEND_CASE(128, 32, 128)
+  LG_APPEND_CASE(128, 64, 256)
+  LG_APPEND_CASE(128, 128, 256)
+  LG_APPEND_CASE(64, 16, 128)
+  LG_APPEND_CASE(64, 32, 128)
+  LG_APPEND_CASE(64, 64, 128)
+  LG_APPEND_CASE(64, 128, 256)
 #undef LG_APPEND_CASE
   return LG_ERR_UNSUPPORTED;
 }

@@ -36,9 +36,9 @@ __host__ __device__ __forceinline__ int64_t held_position(int64_t slot, int64_t 
 }
 
 // pages that the cache of a sequence of n tokens takes (n < 0 counts as 0)
-__host__ __device__ __forceinline__ int pages_of(int64_t n, int sink, int window, int page_tokens) {
+__host__ __device__ __forceinline__ int pages_of(int64_t n, int sink, int window, int page_shift) {
   const int64_t cap = static_cast<int64_t>(sink) + window, held = n < 0 ? 0 : n < cap ? n : cap;
-  return static_cast<int>((held + page_tokens - 1) / page_tokens);
+  return static_cast<int>((held + (1 << page_shift) - 1) >> page_shift);
 }
 
 // The pages that a call writes which takes a sequence from n0 to n1 tokens: the slots of the new tokens are up to three

@@ -111,3 +111,14 @@ def test_chunk_limits(lib):
 
 def test_status_string(lib):
     assert "page" in lg.status_string(-7)
+
+
+def test_sizes_beyond_what_is_covered(lib):
+    assert _calls(lib, _good(), T=(1 << 30) + 1)["lg_paged_slot_map"] == UNSUPPORTED
+    assert _calls(lib, _good(B=65536), T=4)["lg_paged_slot_map"] == UNSUPPORTED
+    assert _calls(lib, _good(B=65536), T=4)["lg_paged_gather"] == UNSUPPORTED
+    assert _calls(lib, _good(B=1 << 30, window_tokens=1 << 20), T=1 << 20)["lg_paged_append"] == UNSUPPORTED
+    # one sequence of more tiles than the decode counts
+    long = _good(B=1, Hq=256, Hkv=256, window_tokens=(1 << 30) - 64, num_pages=10)
+    assert lib.lg_paged_decode_workspace_bytes(C.byref(long)) == 0
+    assert _calls(lib, long)["lg_paged_decode"] == UNSUPPORTED

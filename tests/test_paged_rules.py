@@ -38,7 +38,7 @@ int main() {
     if (t.total() != (int)pages.size() || t.total() > max_touched_pages(T, sink, window, P)) { std::printf("count\n"); return 1; }
     int x = 0;
     for (int p : pages) if (t.page(x++) != p) { std::printf("page\n"); return 1; }
-    if (pages_of(n1, sink, window, P) != (int)((held.size() + P - 1) / P)) { std::printf("pages_of\n"); return 1; }
+    if (pages_of(n1, sink, window, shift) != (int)((held.size() + P - 1) / P)) { std::printf("pages_of\n"); return 1; }
   }
   // far positions: 64-bit counts, on both sides of 2^32 and far behind
   for (const int64_t far : {(1ll << 32) - 150, (1ll << 32) + 3, (1ll << 40) + 12345}) {
@@ -49,7 +49,7 @@ int main() {
     const TouchedPages t = touched_pages(far, far + 1, ring_head(far + 1, 7, 300), 7, 300, 6);
     if (t.total() != 1 || t.page(0) != slot_of(far, 7, 300) / 64) { std::printf("far pages\n"); return 1; }
   }
-  if (pages_of(-5, 4, 100, 16) != 0) { std::printf("negative\n"); return 1; }
+  if (pages_of(-5, 4, 100, 4) != 0) { std::printf("negative\n"); return 1; }
   // exponents: the smallest one that covers, over all magnitudes of bf16 and the borders
   for (uint32_t b = 0; b < 0x7f80u; ++b) {
     uint32_t bits = b << 16;
