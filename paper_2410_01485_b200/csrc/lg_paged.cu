@@ -608,7 +608,7 @@ static __device__ __noinline__ int2 left_out(int64_t n, int C, int sink, int blo
 __device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + fast_log2(l)) * 0.6931471805599453f : -INFINITY; }
 
 // The records of a unit, one per CTA from first_cta on, merged in that order into o and lse: a warp per head, a lane per record's weight.
-// The records sit in the L2: their values travel in batches of eight, the first together with the weights.
+// The records sit in the L2: their values travel in batches of sixteen, the first together with the weights.
 template <int D>
 __device__ __forceinline__ void merge_records(const PagedDecodeArgs& a, const TilePos& p, int u, int first_cta, int n_rec) {
   constexpr int V = D / 32;                  // values of a lane
@@ -620,38 +620,41 @@ __device__ __forceinline__ void merge_records(const PagedDecodeArgs& a, const Ti
     return i < n_rec ? __ldcg(reinterpret_cast<const float2*>(recs + static_cast<int64_t>(i) * (kDecHeads * (D + 2)) + kDecHeads * D) + head)
                      : make_float2(-INFINITY, 0.f);
   };
-  float m = -INFINITY, l = 0.f, acc[V] = {};
+  constexpr int kBatch = 16;
+  float v[kBatch][V];
+  auto load = [&](int i0) {                  // (past the end: the last one, with a weight of zero)
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      const float* src = mine + static_cast<int64_t>(min(i0 + x, n_rec - 1)) * (kDecHeads * (D + 2));
+      if (V == 4) {
+        const float4 t = __ldcg(reinterpret_cast<const float4*>(src));
+        v[x][0] = t.x; v[x][1] = t.y; v[x][V - 2] = t.z; v[x][V - 1] = t.w;
+      } else {
+        const float2 t = __ldcg(reinterpret_cast<const float2*>(src));
+        v[x][0] = t.x; v[x][1] = t.y;
+      }
+    }
+  };
+  float2 ml = pair(lane);
+  load(0);
+  float m = ml.x, l = 0.f, acc[V] = {};
 #pragma unroll 1
-  for (int i = lane; i < n_rec + lane; i += 32) m = fmaxf(m, pair(i).x);
+  for (int i = 32; i < n_rec; i += 32) m = fmaxf(m, pair(i + lane).x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   const float mu = m == -INFINITY ? 0.f : m;
 #pragma unroll 1
-  for (int i0 = 0; i0 < n_rec; i0 += 32) {
-    const float2 ml = pair(i0 + lane);
+  for (int i = 0; i < n_rec; i += kBatch) {
+    if (i > 0) load(i);
+    if (i % 32 == 0 && i > 0) ml = pair(i + lane);
     const float f = fast_exp2(ml.x - mu);
-    l += f * ml.y;
-#pragma unroll 1
-    for (int i = i0; i < min(n_rec, i0 + 32); i += 8) {
-      float v[8][V];
+    if (i % 32 == 0) l += f * ml.y;
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const float* src = mine + static_cast<int64_t>(min(i + x, n_rec - 1)) * (kDecHeads * (D + 2));
-        if (V == 4) {
-          const float4 t = __ldcg(reinterpret_cast<const float4*>(src));
-          v[x][0] = t.x; v[x][1] = t.y; v[x][V - 2] = t.z; v[x][V - 1] = t.w;
-        } else {
-          const float2 t = __ldcg(reinterpret_cast<const float2*>(src));
-          v[x][0] = t.x; v[x][1] = t.y;
-        }
-      }
+    for (int x = 0; x < kBatch; ++x) {
+      const float fx = __shfl_sync(0xffffffffu, f, (i + x) & 31);
+      const float w = i + x < n_rec ? fx : 0.f;
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const float fx = __shfl_sync(0xffffffffu, f, (i + x) & 31);
-        if (i + x >= n_rec) continue;
-#pragma unroll
-        for (int z = 0; z < V; ++z) acc[z] += fx * v[x][z];
-      }
+      for (int z = 0; z < V; ++z) acc[z] += i + x < n_rec ? w * v[x][z] : 0.f;
     }
   }
 #pragma unroll
@@ -837,189 +840,189 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
   int slot = 0, scale_at = 0;
   const int frag_row = ((lane >> 3) & 1) * 8 + (lane & 7);
   auto next_slot = [&]() { slot = slot == SM::kRing - SM::kSlot ? 0 : slot + SM::kSlot; };
-  // (three rounds ahead of the first tile only ask: a second copy of that code in front of the loop would have to be fetched)
+  // three tiles' K and two tiles' V (straight code: at the start what counts is the jumps to code that was not fetched yet)
+#pragma unroll
+  for (int x = 0; x < 3; ++x) {
+    if (x < n_run) { ask_k(); copy_tile(a.pool[0]); }
+    copy_commit();
+    if (x == 2) break;
+    if (x < n_run) copy_tile(a.pool[1]);
+    copy_commit();
+  }
 #pragma unroll 1
-  for (int i = -3; i < n_run || i < 0; ++i) {
+  for (int i = 0; i < n_run; ++i) {
     float s[2][4] = {};
-    float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);   // (K, V) scale of the tile's first half, of its second
-    bool in0 = false, in1 = false, edge = false;
     const int first_slot = cur.t * kPagedTile;
-    if (i >= 0) {
-      if (i == 0 || cur.t == 0) {
-        // A unit begins.  q in f16, its row scaled by a power of two to at most 2^11: b0 = dims 16 k + 4 c, +1, b1 = the next two (the
-        // pieces of a row that ldmatrix hands to a thread are four neighbouring bytes, and the order of a product's terms is free).
-        if (i > 0) load_q(cur);
-        nvalid = valid_of(cur);
-        ex_cnt = 0;
-        if (a.block_tokens > 0) {
-          const int2 x = left_out(a.n_tokens[cur.b], a.C, a.sink, a.block_tokens);
-          ex0 = x.x; ex_cnt = x.y;
-        }
-        uint32_t top = 0;                     // magnitudes of finite values
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            uint32_t w = (j ? qw[k].y : qw[k].x) & 0x7fff7fffu;
-            w &= ~__vcmpgeu2(w, 0x7f807f80u);
-            top = __vmaxu2(top, w);
-          }
-        }
-        top = max(top >> 16, top & 0xffffu);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const int e = top == 0 ? 0 : min(126, 137 - static_cast<int>(top >> 7));   // the largest value becomes 2^10 to 2^11
-        const float mul = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
-        const float q_mul = __uint_as_float(static_cast<uint32_t>(127 - e) << 23) * a.scale_log2;
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          qf[k][0] = pack_f16(bf16_lo(qw[k].x) * mul, bf16_hi(qw[k].x) * mul);
-          qf[k][1] = pack_f16(bf16_lo(qw[k].y) * mul, bf16_hi(qw[k].y) * mul);
-        }
-        qs0 = __shfl_sync(0xffffffffu, q_mul, 8 * c);
-        qs1 = __shfl_sync(0xffffffffu, q_mul, 8 * c + 4);
-        m_run[0] = m_run[1] = r_run[0] = r_run[1] = -INFINITY;
-        l_run[0] = l_run[1] = 0.f;
-#pragma unroll
-        for (int x = 0; x < D / 16; ++x) oacc[x][0] = oacc[x][1] = oacc[x][2] = oacc[x][3] = 0.f;
-        same = true;
-        vs_ref = -1.f;
-        first_t = cur.t;
+    if (i == 0 || cur.t == 0) {
+      // A unit begins.  q in f16, its row scaled by a power of two to at most 2^11: b0 = dims 16 k + 4 c, +1, b1 = the next two (the
+      // pieces of a row that ldmatrix hands to a thread are four neighbouring bytes, and the order of a product's terms is free).
+      if (i > 0) load_q(cur);
+      nvalid = valid_of(cur);
+      ex_cnt = 0;
+      if (a.block_tokens > 0) {
+        const int2 x = left_out(a.n_tokens[cur.b], a.C, a.sink, a.block_tokens);
+        ex0 = x.x; ex_cnt = x.y;
       }
-      copy_wait<kPagedSlots - 1>();
-      __syncwarp();                           // K of the tile and its scales are there
-      sc = *reinterpret_cast<const float4*>(sm + SM::kScales + warp * 48 + scale_at);
-      scale_at = scale_at == 32 ? 0 : scale_at + 16;
-      in0 = sc.y >= 0.f; in1 = sc.w >= 0.f;
-      edge = first_slot + kPagedTile > nvalid || !in0 || !in1;
-      if (ex_cnt > 0 && first_slot + kPagedTile > a.sink) {
-        int d = max(first_slot, a.sink) - a.sink - ex0;  // the tile's first ring slot from the first one left out
-        if (d < 0) d += ring_w;
-        edge |= d < ex_cnt || d + kPagedTile > ring_w;
+      uint32_t top = 0;                     // magnitudes of finite values
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          uint32_t w = (j ? qw[k].y : qw[k].x) & 0x7fff7fffu;
+          w &= ~__vcmpgeu2(w, 0x7f807f80u);
+          top = __vmaxu2(top, w);
+        }
       }
+      top = max(top >> 16, top & 0xffffu);
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int e = top == 0 ? 0 : min(126, 137 - static_cast<int>(top >> 7));   // the largest value becomes 2^10 to 2^11
+      const float mul = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+      const float q_mul = __uint_as_float(static_cast<uint32_t>(127 - e) << 23) * a.scale_log2;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        qf[k][0] = pack_f16(bf16_lo(qw[k].x) * mul, bf16_hi(qw[k].x) * mul);
+        qf[k][1] = pack_f16(bf16_lo(qw[k].y) * mul, bf16_hi(qw[k].y) * mul);
+      }
+      qs0 = __shfl_sync(0xffffffffu, q_mul, 8 * c);
+      qs1 = __shfl_sync(0xffffffffu, q_mul, 8 * c + 4);
+      m_run[0] = m_run[1] = r_run[0] = r_run[1] = -INFINITY;
+      l_run[0] = l_run[1] = 0.f;
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x) oacc[x][0] = oacc[x][1] = oacc[x][2] = oacc[x][3] = 0.f;
+      same = true;
+      vs_ref = -1.f;
+      first_t = cur.t;
+    }
+    copy_wait<kPagedSlots - 1>();
+    __syncwarp();                           // K of the tile and its scales are there
+    const float4 sc = *reinterpret_cast<const float4*>(sm + SM::kScales + warp * 48 + scale_at);   // (K, V) scale of the first half, of the second
+    scale_at = scale_at == 32 ? 0 : scale_at + 16;
+    const bool in0 = sc.y >= 0.f, in1 = sc.w >= 0.f;
+    bool edge = first_slot + kPagedTile > nvalid || !in0 || !in1;
+    if (ex_cnt > 0 && first_slot + kPagedTile > a.sink) {
+      int d = max(first_slot, a.sink) - a.sink - ex0;  // the tile's first ring slot from the first one left out
+      if (d < 0) d += ring_w;
+      edge |= d < ex_cnt || d + kPagedTile > ring_w;
+    }
 
-      // ---- S^T[32 tokens, 8 heads] = K Q^T
-      const uint32_t sk = ring + slot;
+    // ---- S^T[32 tokens, 8 heads] = K Q^T
+    const uint32_t sk = ring + slot;
 #pragma unroll
-      for (int k = 0; k < D / 16; k += 2) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          uint32_t x0, x1, x2, x3;            // rows 0-7 and 8-15 of chunk k, the same of chunk k + 1
-          ldsm_x4(sk + tile_offset<D>(16 * x + frag_row, k + (lane >> 4)), x0, x1, x2, x3);
-          mma16816_f16(s[x], e4m3x2_to_f16x2(x0), e4m3x2_to_f16x2(x1), e4m3x2_hi_to_f16x2(x0), e4m3x2_hi_to_f16x2(x1), qf[k][0], qf[k][1]);
-          mma16816_f16(s[x], e4m3x2_to_f16x2(x2), e4m3x2_to_f16x2(x3), e4m3x2_hi_to_f16x2(x2), e4m3x2_hi_to_f16x2(x3), qf[k + 1][0], qf[k + 1][1]);
-        }
-      }
-      next_slot();
-      __syncwarp();                           // K has been read
-    }
-    if (i > -3) {
-      if (i + 2 < n_run) copy_tile(a.pool[1]);   // V of the tile whose K was asked for last
-      copy_commit();
-    }
-    if (i >= 0) {
-      // s[x][0, 1]: token 16 x + r, heads 2c, 2c+1; s[x][2, 3]: token 16 x + r + 8.  (The scales together are kept finite: a score of
-      // zero stays zero.)
+    for (int k = 0; k < D / 16; k += 2) {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const float kk = x ? sc.z : sc.x, c0 = fminf(qs0 * kk, 3.4e38f), c1 = fminf(qs1 * kk, 3.4e38f);
-        s[x][0] *= c0; s[x][1] *= c1; s[x][2] *= c0; s[x][3] *= c1;
+        uint32_t x0, x1, x2, x3;            // rows 0-7 and 8-15 of chunk k, the same of chunk k + 1
+        ldsm_x4(sk + tile_offset<D>(16 * x + frag_row, k + (lane >> 4)), x0, x1, x2, x3);
+        mma16816_f16(s[x], e4m3x2_to_f16x2(x0), e4m3x2_to_f16x2(x1), e4m3x2_hi_to_f16x2(x0), e4m3x2_hi_to_f16x2(x1), qf[k][0], qf[k][1]);
+        mma16816_f16(s[x], e4m3x2_to_f16x2(x2), e4m3x2_to_f16x2(x3), e4m3x2_hi_to_f16x2(x2), e4m3x2_hi_to_f16x2(x3), qf[k + 1][0], qf[k + 1][1]);
       }
-      if (edge) {
+    }
+    next_slot();
+    __syncwarp();                           // K has been read
+    if (i + 2 < n_run) copy_tile(a.pool[1]);   // V of the tile whose K was asked for last
+    copy_commit();
+
+    // s[x][0, 1]: token 16 x + r, heads 2c, 2c+1; s[x][2, 3]: token 16 x + r + 8.  (The scales together are kept finite: a score of
+    // zero stays zero.)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const bool in = x ? in1 : in0;
-          if (!in || !attended(first_slot + 16 * x + r)) s[x][0] = s[x][1] = -INFINITY;
-          if (!in || !attended(first_slot + 16 * x + r + 8)) s[x][2] = s[x][3] = -INFINITY;
-        }
+    for (int x = 0; x < 2; ++x) {
+      const float kk = x ? sc.z : sc.x, c0 = fminf(qs0 * kk, 3.4e38f), c1 = fminf(qs1 * kk, 3.4e38f);
+      s[x][0] *= c0; s[x][1] *= c1; s[x][2] *= c0; s[x][3] *= c1;
+    }
+    if (edge) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const bool in = x ? in1 : in0;
+        if (!in || !attended(first_slot + 16 * x + r)) s[x][0] = s[x][1] = -INFINITY;
+        if (!in || !attended(first_slot + 16 * x + r + 8)) s[x][2] = s[x][3] = -INFINITY;
       }
-      float t0 = fmaxf(fmaxf(s[0][0], s[0][2]), fmaxf(s[1][0], s[1][2])), t1 = fmaxf(fmaxf(s[0][1], s[0][3]), fmaxf(s[1][1], s[1][3]));
+    }
+    float t0 = fmaxf(fmaxf(s[0][0], s[0][2]), fmaxf(s[1][0], s[1][2])), t1 = fmaxf(fmaxf(s[0][1], s[0][3]), fmaxf(s[1][1], s[1][3]));
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, o));
+      t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, o));
+    }
+    const float mn0 = fmaxf(m_run[0], t0), mn1 = fmaxf(m_run[1], t1);
+    const float mu0 = mn0 == -INFINITY ? 0.f : mn0, mu1 = mn1 == -INFINITY ? 0.f : mn1;
+    float be0 = fast_exp2(m_run[0] - mu0), be1 = fast_exp2(m_run[1] - mu1);
+    float w[2][4];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      w[x][0] = fast_exp2(s[x][0] - mu0); w[x][1] = fast_exp2(s[x][1] - mu1);
+      w[x][2] = fast_exp2(s[x][2] - mu0); w[x][3] = fast_exp2(s[x][3] - mu1);
+    }
+    l_run[0] = l_run[0] * be0 + ((w[0][0] + w[0][2]) + (w[1][0] + w[1][2]));
+    l_run[1] = l_run[1] * be1 + ((w[0][1] + w[0][3]) + (w[1][1] + w[1][3]));
+    const float v0 = in0 ? sc.y : in1 ? sc.w : vs_ref, v1 = in1 ? sc.w : v0;   // (a half that is not there has no weights)
+    if (vs_ref < 0.f) vs_ref = v0;
+    if (same && (v0 != vs_ref || v1 != vs_ref)) {   // from here on the weights have a reference of their own
+      same = false;
+      const float lr = fast_log2(vs_ref);
+      r_run[0] = m_run[0] + lr; r_run[1] = m_run[1] + lr;
+    }
+    m_run[0] = mn0; m_run[1] = mn1;
+    if (!same) {
+      const float lv0 = fast_log2(v0), lv1 = fast_log2(v1);
+      float u0 = fmaxf(fmaxf(s[0][0], s[0][2]) + lv0, fmaxf(s[1][0], s[1][2]) + lv1);
+      float u1 = fmaxf(fmaxf(s[0][1], s[0][3]) + lv0, fmaxf(s[1][1], s[1][3]) + lv1);
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) {
-        t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, o));
-        t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, o));
+        u0 = fmaxf(u0, __shfl_xor_sync(0xffffffffu, u0, o));
+        u1 = fmaxf(u1, __shfl_xor_sync(0xffffffffu, u1, o));
       }
-      const float mn0 = fmaxf(m_run[0], t0), mn1 = fmaxf(m_run[1], t1);
-      const float mu0 = mn0 == -INFINITY ? 0.f : mn0, mu1 = mn1 == -INFINITY ? 0.f : mn1;
-      float be0 = fast_exp2(m_run[0] - mu0), be1 = fast_exp2(m_run[1] - mu1);
-      float w[2][4];
+      const float rn0 = fmaxf(r_run[0], u0), rn1 = fmaxf(r_run[1], u1);
+      const float ru0 = rn0 == -INFINITY ? 0.f : rn0, ru1 = rn1 == -INFINITY ? 0.f : rn1;
+      be0 = fast_exp2(r_run[0] - ru0); be1 = fast_exp2(r_run[1] - ru1);
+      r_run[0] = rn0; r_run[1] = rn1;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        w[x][0] = fast_exp2(s[x][0] - mu0); w[x][1] = fast_exp2(s[x][1] - mu1);
-        w[x][2] = fast_exp2(s[x][2] - mu0); w[x][3] = fast_exp2(s[x][3] - mu1);
+        const float d0 = (x ? lv1 : lv0) - ru0, d1 = (x ? lv1 : lv0) - ru1;
+        w[x][0] = fast_exp2(s[x][0] + d0); w[x][1] = fast_exp2(s[x][1] + d1);
+        w[x][2] = fast_exp2(s[x][2] + d0); w[x][3] = fast_exp2(s[x][3] + d1);
       }
-      l_run[0] = l_run[0] * be0 + ((w[0][0] + w[0][2]) + (w[1][0] + w[1][2]));
-      l_run[1] = l_run[1] * be1 + ((w[0][1] + w[0][3]) + (w[1][1] + w[1][3]));
-      const float v0 = in0 ? sc.y : in1 ? sc.w : vs_ref, v1 = in1 ? sc.w : v0;   // (a half that is not there has no weights)
-      if (vs_ref < 0.f) vs_ref = v0;
-      if (same && (v0 != vs_ref || v1 != vs_ref)) {   // from here on the weights have a reference of their own
-        same = false;
-        const float lr = fast_log2(vs_ref);
-        r_run[0] = m_run[0] + lr; r_run[1] = m_run[1] + lr;
-      }
-      m_run[0] = mn0; m_run[1] = mn1;
-      if (!same) {
-        const float lv0 = fast_log2(v0), lv1 = fast_log2(v1);
-        float u0 = fmaxf(fmaxf(s[0][0], s[0][2]) + lv0, fmaxf(s[1][0], s[1][2]) + lv1);
-        float u1 = fmaxf(fmaxf(s[0][1], s[0][3]) + lv0, fmaxf(s[1][1], s[1][3]) + lv1);
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) {
-          u0 = fmaxf(u0, __shfl_xor_sync(0xffffffffu, u0, o));
-          u1 = fmaxf(u1, __shfl_xor_sync(0xffffffffu, u1, o));
-        }
-        const float rn0 = fmaxf(r_run[0], u0), rn1 = fmaxf(r_run[1], u1);
-        const float ru0 = rn0 == -INFINITY ? 0.f : rn0, ru1 = rn1 == -INFINITY ? 0.f : rn1;
-        be0 = fast_exp2(r_run[0] - ru0); be1 = fast_exp2(r_run[1] - ru1);
-        r_run[0] = rn0; r_run[1] = rn1;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const float d0 = (x ? lv1 : lv0) - ru0, d1 = (x ? lv1 : lv0) - ru1;
-          w[x][0] = fast_exp2(s[x][0] + d0); w[x][1] = fast_exp2(s[x][1] + d1);
-          w[x][2] = fast_exp2(s[x][2] + d0); w[x][3] = fast_exp2(s[x][3] + d1);
-        }
-      }
-      if (__any_sync(0xffffffffu, be0 != 1.f || be1 != 1.f)) {
-#pragma unroll
-        for (int x = 0; x < D / 16; ++x) { oacc[x][0] *= be0; oacc[x][1] *= be1; oacc[x][2] *= be0; oacc[x][3] *= be1; }
-      }
-      uint32_t pb[2][2];                      // P^T as the B operand: tokens 2c, +1 of head r, then 8 + 2c, +1
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        pb[x][0] = movmatrix_t(pack_f16(w[x][0], w[x][1]));
-        pb[x][1] = movmatrix_t(pack_f16(w[x][2], w[x][3]));
-      }
-
-      copy_wait<kPagedSlots - 1>();
-      __syncwarp();                           // V of the tile is there
-      const uint32_t sv = ring + slot;
-      if (edge) {   // rows that are not attended hold anything at all: a weight of zero does not silence a NaN of V, so those rows are zeroed
-        if (!((lane < kPagedHalf ? in0 : in1) && attended(first_slot + lane))) {
-#pragma unroll
-          for (int x = 0; x < D / 16; ++x)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sv + lane * D + x * 16), "r"(0) : "memory");
-        }
-        __syncwarp();
-      }
-      // ---- O^T[D, 8 heads] += V^T P^T.  Transposed, a thread's 32 bits are dims 2r, 2r+1 of tokens 2c and 2c+1: the even dims are
-      // the product's rows 0-7, the odd ones its rows 8-15.
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-#pragma unroll
-        for (int k = 0; k < D / 16; k += 2) {
-          uint32_t x0, x1, x2, x3;            // tokens 0-7 and 8-15 of chunk k, the same of chunk k + 1
-          ldsm_x4_t(sv + tile_offset<D>(16 * x + frag_row, k + (lane >> 4)), x0, x1, x2, x3);
-          x0 = __byte_perm(x0, 0, 0x3120); x1 = __byte_perm(x1, 0, 0x3120);
-          x2 = __byte_perm(x2, 0, 0x3120); x3 = __byte_perm(x3, 0, 0x3120);
-          mma16816_f16(oacc[k], e4m3x2_to_f16x2(x0), e4m3x2_hi_to_f16x2(x0), e4m3x2_to_f16x2(x1), e4m3x2_hi_to_f16x2(x1), pb[x][0], pb[x][1]);
-          mma16816_f16(oacc[k + 1], e4m3x2_to_f16x2(x2), e4m3x2_hi_to_f16x2(x2), e4m3x2_to_f16x2(x3), e4m3x2_hi_to_f16x2(x3), pb[x][0], pb[x][1]);
-        }
-      }
-      next_slot();
-      __syncwarp();                           // V has been read
     }
+    if (__any_sync(0xffffffffu, be0 != 1.f || be1 != 1.f)) {
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x) { oacc[x][0] *= be0; oacc[x][1] *= be1; oacc[x][2] *= be0; oacc[x][3] *= be1; }
+    }
+    uint32_t pb[2][2];                      // P^T as the B operand: tokens 2c, +1 of head r, then 8 + 2c, +1
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      pb[x][0] = movmatrix_t(pack_f16(w[x][0], w[x][1]));
+      pb[x][1] = movmatrix_t(pack_f16(w[x][2], w[x][3]));
+    }
+
+    copy_wait<kPagedSlots - 1>();
+    __syncwarp();                           // V of the tile is there
+    const uint32_t sv = ring + slot;
+    if (edge) {   // rows that are not attended hold anything at all: a weight of zero does not silence a NaN of V, so those rows are zeroed
+      if (!((lane < kPagedHalf ? in0 : in1) && attended(first_slot + lane))) {
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x)
+          asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sv + lane * D + x * 16), "r"(0) : "memory");
+      }
+      __syncwarp();
+    }
+    // ---- O^T[D, 8 heads] += V^T P^T.  Transposed, a thread's 32 bits are dims 2r, 2r+1 of tokens 2c and 2c+1: the even dims are
+    // the product's rows 0-7, the odd ones its rows 8-15.
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+      for (int k = 0; k < D / 16; k += 2) {
+        uint32_t x0, x1, x2, x3;            // tokens 0-7 and 8-15 of chunk k, the same of chunk k + 1
+        ldsm_x4_t(sv + tile_offset<D>(16 * x + frag_row, k + (lane >> 4)), x0, x1, x2, x3);
+        x0 = __byte_perm(x0, 0, 0x3120); x1 = __byte_perm(x1, 0, 0x3120);
+        x2 = __byte_perm(x2, 0, 0x3120); x3 = __byte_perm(x3, 0, 0x3120);
+        mma16816_f16(oacc[k], e4m3x2_to_f16x2(x0), e4m3x2_hi_to_f16x2(x0), e4m3x2_to_f16x2(x1), e4m3x2_hi_to_f16x2(x1), pb[x][0], pb[x][1]);
+        mma16816_f16(oacc[k + 1], e4m3x2_to_f16x2(x2), e4m3x2_hi_to_f16x2(x2), e4m3x2_to_f16x2(x3), e4m3x2_hi_to_f16x2(x3), pb[x][0], pb[x][1]);
+      }
+    }
+    next_slot();
+    __syncwarp();                           // V has been read
     if (i + 3 < n_run) { ask_k(); copy_tile(a.pool[0]); }
     copy_commit();
-    if (i < 0) continue;
     ++cur.t;
     const bool tail = cur.t == cur.nt;
     if (tail || i + 1 == n_run) {
@@ -1082,19 +1085,15 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
     float l = f * ml.y, acc[D / 32] = {};
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-#pragma unroll 1
-    for (unsigned rest = mask; rest != 0;) {  // two at a time
-      const int y = __ffs(rest) - 1, later = __ffs(rest & (rest - 1)) - 1, z = later < 0 ? y : later;
-      rest &= rest - 1;
-      rest &= rest - 1;
-      const float fy = __shfl_sync(0xffffffffu, f, y), fz = later < 0 ? 0.f : __shfl_sync(0xffffffffu, f, z);
-      const float *p = piece_at(y) + lane * 2, *q = piece_at(z) + lane * 2;
+#pragma unroll
+    for (int y = 0; y < 2 * kDecWarps; ++y) {
+      const float fy = __shfl_sync(0xffffffffu, f, y);
+      if (!(mask >> y & 1)) continue;
 #pragma unroll
       for (int x = 0; x < D / 32; x += 2) {
-        const float2 v = *reinterpret_cast<const float2*>(p + 32 * x), w = *reinterpret_cast<const float2*>(q + 32 * x);
+        const float2 v = *reinterpret_cast<const float2*>(piece_at(y) + lane * 2 + 32 * x);
         acc[x] += fy * v.x;
         acc[x + 1] += fy * v.y;
-        if (later >= 0) { acc[x] += fz * w.x; acc[x + 1] += fz * w.y; }
       }
     }
     if ((u == sh0.x && sh0.z > 1) || (u == sh1.x && sh1.z > 1)) {
