@@ -838,8 +838,8 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
   int slot = 0, scale_at = 0;
   const int frag_row = ((lane >> 3) & 1) * 8 + (lane & 7);
   auto next_slot = [&]() { slot = slot == SM::kRing - SM::kSlot ? 0 : slot + SM::kSlot; };
-  // three tiles' K and two tiles' V (straight code: at the start what counts is the jumps to code that was not fetched yet)
-#pragma unroll
+  // three tiles' K and two tiles' V
+#pragma unroll 1
   for (int x = 0; x < 3; ++x) {
     if (x < n_run) { ask_k(); copy_tile(a.pool[0]); }
     copy_commit();
@@ -1064,7 +1064,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
   if (lane == 0) { meta[2 * warp] = piece[0]; meta[2 * warp + 1] = piece[1]; }
   __syncthreads();
 
-  // ---- the pieces of my CTA's warps, unit by unit (a warp per head, a lane per piece's weight); what is not a whole unit becomes a record
+  // ---- the pieces of my CTA's warps, unit by unit (a warp per head); what is not a whole unit becomes a record
   const int4 mine_of = lane < 2 * kDecWarps ? meta[lane] : make_int4(-1, 0, 0, 0);
   const int4 sh0 = reinterpret_cast<const int4*>(sm + SM::kShare)[0], sh1 = reinterpret_cast<const int4*>(sm + SM::kShare)[2];
   const float* heads = reinterpret_cast<const float*>(sm) + warp * (D + 2);
@@ -1074,24 +1074,22 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
     const int y0 = __ffs(left) - 1, u = __shfl_sync(0xffffffffu, mine_of.x, y0);
     const unsigned mask = __ballot_sync(0xffffffffu, mine_of.x == u);
     left &= ~mask;
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (mask >> lane & 1) ml = *reinterpret_cast<const float2*>(piece_at(lane) + D);
-    float m = ml.x;
+    float2 ml[2 * kDecWarps];
+    float m = -INFINITY, l = 0.f, acc[D / 32] = {};
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float f = fast_exp2(ml.x - (m == -INFINITY ? 0.f : m));
-    float l = f * ml.y, acc[D / 32] = {};
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    for (int y = 0; y < 2 * kDecWarps; ++y)
+      if (mask >> y & 1) { ml[y] = *reinterpret_cast<const float2*>(piece_at(y) + D); m = fmaxf(m, ml[y].x); }
+    const float mu = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int y = 0; y < 2 * kDecWarps; ++y) {
-      const float fy = __shfl_sync(0xffffffffu, f, y);
       if (!(mask >> y & 1)) continue;
+      const float f = fast_exp2(ml[y].x - mu);
+      l += f * ml[y].y;
 #pragma unroll
       for (int x = 0; x < D / 32; x += 2) {
         const float2 v = *reinterpret_cast<const float2*>(piece_at(y) + lane * 2 + 32 * x);
-        acc[x] += fy * v.x;
-        acc[x + 1] += fy * v.y;
+        acc[x] += f * v.x;
+        acc[x + 1] += f * v.y;
       }
     }
     if ((u == sh0.x && sh0.z > 1) || (u == sh1.x && sh1.z > 1)) {
