@@ -9,6 +9,7 @@
 #include "lg_common.cuh"
 #include "lg_host.h"
 #include "lg_index.cuh"
+#include "lg_paged.cuh"
 
 namespace lg {
 
@@ -389,6 +390,38 @@ static lg_status plan_chunk(const lg_decode_params* p, int32_t T, int64_t n_befo
   return LG_OK;
 }
 
+// ---- a chunk served against the paged cache ---------------------------------------------------
+// One launch ahead of the attention kernel: block 0 builds the forward's schedule (a warp per super-tile, then their ranks, as
+// sched_build_kernel and sched_order_kernel do) and checks the tables, the other blocks copy (paged_linearise).  Block 0 alone writes the header, so that
+// what it finds missing is not wiped.
+constexpr int kChunkMaxTiles = 64;   // super-tiles that one block ranks; longer chunks have their schedule built by the two launches
+__global__ void __launch_bounds__(kGatherThreads) chunk_prepare_kernel(const SchedArgs a, const PagedLinearise l, int blocks_x, int build) {
+  pdl_trigger();
+  pdl_wait();
+  if (blockIdx.x > 0) {
+    const int64_t w = blockIdx.x - 1, bh = w / blocks_x;
+    const int b = static_cast<int>(bh / l.Hkv);
+    paged_linearise(l, (w - bh * blocks_x) * kGatherThreads + threadIdx.x, static_cast<int>(bh - static_cast<int64_t>(b) * l.Hkv), b);
+    return;
+  }
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (build) {
+    if (threadIdx.x == 0) header_begin(a.header);
+    for (int t = warp; t < a.n_stiles; t += kGatherThreads / 32) {
+      const int r0 = a.st_row0 + 2 * a.R * t, off = row_start(a.p, r0) - row_start(a.p, a.st_row0);
+      const int n = merge_rows(a.p, r0, 2 * a.R, 16, a.sq_ent + off);
+      if (lane == 0) { a.sq_off[t] = off; a.sq_cnt[t] = n; }
+    }
+  }
+  const bool missing = paged_entry_missing(l, kGatherThreads);   // (its barrier also stands between the counts and the ranks)
+  if (missing && threadIdx.x == 0) atomicCAS(l.error_word, 0u, kPageError);
+  if (!build) return;
+  for (int t = warp; t < a.n_stiles; t += kGatherThreads / 32) {
+    const int rank = rank_of(a.sq_cnt, a.n_stiles, t);
+    if (lane == 0) a.sq_order[rank] = TileRec{a.sq_off[t], a.sq_cnt[t], t, -1};
+  }
+}
+
 // ---- self-test of the bounded wait -----------------------------------------------------------
 // One thread waits on a barrier nobody will ever arrive at, with a limit of about a millisecond:
 // the wait gives up, records its site in the error word and the kernel ends normally.
@@ -703,7 +736,15 @@ lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, 
     ChunkPlan c;
     if ((s = plan_chunk(&d, T, n, &c)) != LG_OK) return s;
     c.r.max_prob = kChunkMaxProb;
-    if ((s = prepare_workspace(c.r, c.w, ws, 1, true, 0, st)) != LG_OK) return s;
+    const bool one = c.r.n_stiles <= kChunkMaxTiles;
+    if (!one && (s = prepare_workspace(c.r, c.w, ws, 1, true, 0, st)) != LG_OK) return s;
+    SchedArgs sched{};
+    sched.p = c.r.pat;
+    sched.header = reinterpret_cast<WsHeader*>(ws);
+    sched.R = 128 / c.r.block;
+    sched.n_stiles = c.r.n_stiles; sched.st_row0 = c.r.st_row0;
+    sched.sq_off = reinterpret_cast<int32_t*>(ws + c.w.sq_off); sched.sq_cnt = reinterpret_cast<int32_t*>(ws + c.w.sq_cnt);
+    sched.sq_ent = reinterpret_cast<int32_t*>(ws + c.w.sq_ent); sched.sq_order = reinterpret_cast<TileRec*>(ws + c.w.sq_order);
     PagedLinearise l;
     l.pool[0] = k_pool; l.pool[1] = v_pool; l.scale[0] = k_scale; l.scale[1] = v_scale;
     l.error_word = reinterpret_cast<unsigned int*>(ws);
@@ -711,15 +752,20 @@ lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, 
     l.page_shift = page_shift(p->page_tokens); l.num_pages = p->num_pages; l.stride = stride;
     __nv_bfloat16* lin[2] = {reinterpret_cast<__nv_bfloat16*>(ws + c.o_k), reinterpret_cast<__nv_bfloat16*>(ws + c.o_v)};
     for (int x = b; x < e; x += kLineariseSeqs) {
-      const int m = e - x < kLineariseSeqs ? e - x : kLineariseSeqs;
-      for (int y = 0; y < m; ++y)
+      l.B = e - x < kLineariseSeqs ? e - x : kLineariseSeqs;
+      for (int y = 0; y < l.B; ++y)
         l.ring0[y] = c.kept > p->sink_tokens ? static_cast<int>((n_tokens_before[x + y] - c.kept) % p->window_tokens) : 0;
       for (int y = 0; y < 2; ++y) {
         l.chunk[y] = static_cast<const __nv_bfloat16*>(y ? v_chunk : k_chunk) + static_cast<int64_t>(x) * p->Hkv * T * p->D;
         l.lin[y] = lin[y] + static_cast<int64_t>(x - b) * p->Hkv * c.ap.L * p->D;
       }
       l.table = block_table + static_cast<int64_t>(x) * stride;
-      if ((s = launch_paged_linearise(l, m, st)) != LG_OK) return s;
+      const int64_t blocks_x = (static_cast<int64_t>(c.ap.L) * (p->D / 16) + kGatherThreads - 1) / kGatherThreads;
+      const int64_t blocks = blocks_x * p->Hkv * l.B + 1;
+      if (blocks > 0x7fffffff) return LG_ERR_UNSUPPORTED;
+      if (launch_kernel(true, chunk_prepare_kernel, dim3(static_cast<unsigned>(blocks)), kGatherThreads, 0, st, sched, l, static_cast<int>(blocks_x),
+                        one && x == b ? 1 : 0) != cudaSuccess)
+        return LG_ERR_CUDA;
     }
     if ((s = launch_fwd(c.r, c.w, static_cast<const __nv_bfloat16*>(q_chunk) + q_at * p->D, lin[0], lin[1],
                         static_cast<__nv_bfloat16*>(o) + q_at * p->D, lse + q_at, ws, st)) != LG_OK)

@@ -216,17 +216,5 @@ size_t attn_workspace_bytes(const lg_attn_params* p, int want_bwd, int kv_total)
 lg_status check_paged(const lg_paged_params* p);
 int paged_table_stride(const lg_paged_params* p);
 int page_shift(int page_tokens);
-constexpr int kLineariseSeqs = 128;   // sequences of one launch
-struct PagedLinearise {
-  const void* pool[2];       // K, V
-  const float* scale[2];
-  const void* chunk[2];      // [B, Hkv, T, D] bf16
-  void* lin[2];              // [B, Hkv, kept + T, D] bf16
-  const int32_t* table;
-  unsigned int* error_word;
-  int Hkv, D, T, kept, sink, window, page_shift, num_pages, stride;
-  int ring0[kLineariseSeqs]; // ring offset of each sequence's oldest kept token
-};
-lg_status launch_paged_linearise(const PagedLinearise& a, int B /* <= kLineariseSeqs */, cudaStream_t stream);
 
 }  // namespace lg

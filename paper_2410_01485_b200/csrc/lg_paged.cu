@@ -6,41 +6,24 @@
 // rescaled by exponents alone, which is exact but for codes below the normal range (values under 2^-14 of the largest),
 // where scales of amax / 448 would round every token of the page anew with every append.  e4m3 keeps 4 significant bits
 // wherever a value lies in its 15 octaves, so nothing is lost by a scale up to twice as large.
-#include <cuda_fp16.h>
 #include <math.h>
 
 #include "lg_common.cuh"
 #include "lg_decode.cuh"
 #include "lg_host.h"
-#include "lg_paged.h"
+#include "lg_paged.cuh"
 
 namespace lg {
 
 // ---- e4m3 -------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {   // low 16 bits: two codes
-  uint32_t r;
-  asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\t}" : "=r"(r) : "r"(two));
-  return r;
-}
-__device__ __forceinline__ uint32_t e4m3x2_hi_to_f16x2(uint32_t four) {   // high 16 bits
-  uint32_t r;
-  asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, y;\n\t}" : "=r"(r) : "r"(four));
-  return r;
-}
 // Round to nearest even; beyond 448 (infinities) the largest code, NaN stays NaN.
 __device__ __forceinline__ uint32_t f32x2_to_e4m3x2(float lo, float hi) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
-__device__ __forceinline__ float2 f16x2_to_f32x2(uint32_t h) {
-  return __half22float2(*reinterpret_cast<const __half2*>(&h));
-}
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
-// The page of a table entry, or -1 where the entry names no page of the pool.
-__device__ __forceinline__ int checked_page(int page, int num_pages) { return page >= 0 && page < num_pages ? page : -1; }
 
 // ---- block tables and slot maps ------------------------------------------------------------
 // A CTA works `rows` consecutive sequences and kExtendCols table columns of their new pages; where a sequence's pages
@@ -361,13 +344,6 @@ __global__ void __launch_bounds__(kThreads) paged_append_kernel(const AppendArgs
 }
 
 // ---- rows of the cache in bf16 ---------------------------------------------------------------
-// 16 codes times the page's scale (exact for a power-of-two scale: 4 significant bits) as two 16-byte pieces.
-__device__ __forceinline__ void dequant16(uint4 c, float s, uint4& lo, uint4& hi) {
-  auto two = [s](uint32_t h) { const float2 f = f16x2_to_f32x2(h); return pack_bf16(f.x * s, f.y * s); };
-  lo = make_uint4(two(e4m3x2_to_f16x2(c.x)), two(e4m3x2_hi_to_f16x2(c.x)), two(e4m3x2_to_f16x2(c.y)), two(e4m3x2_hi_to_f16x2(c.y)));
-  hi = make_uint4(two(e4m3x2_to_f16x2(c.z)), two(e4m3x2_hi_to_f16x2(c.z)), two(e4m3x2_to_f16x2(c.w)), two(e4m3x2_hi_to_f16x2(c.w)));
-}
-
 struct GatherArgs {
   const uint8_t* pool[2];
   const float* scale[2];
@@ -375,7 +351,6 @@ struct GatherArgs {
   uint4* out[2];             // [B, Hkv, T, D]
   int Hkv, T, D, page_shift, num_pages;
 };
-constexpr int kGatherThreads = 256;
 
 __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const GatherArgs a) {
   pdl_trigger();
@@ -398,58 +373,6 @@ __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const Gath
     a.out[x][to * 2] = lo;
     a.out[x][to * 2 + 1] = hi;
   }
-}
-
-// What a chunk attends to, as one sequence in time order: the `kept` tokens that the cache holds after n tokens (the sink, then
-// the ring from its oldest token on, ring0 of the sequence), then the chunk's own rows.  Rows whose page is absent are zeros and the status
-// word says so: the attention kernel behind then does nothing.
-__global__ void __launch_bounds__(kGatherThreads) paged_linearise_kernel(const PagedLinearise a) {
-  pdl_trigger();
-  const int per_row = a.D / 16, L = a.kept + a.T;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kGatherThreads + threadIdx.x;
-  const int64_t v = i / per_row;
-  const int c = static_cast<int>(i - v * per_row), h = blockIdx.y, b = blockIdx.z;
-  if (v >= L) return;
-  pdl_wait();
-  const int64_t bh = static_cast<int64_t>(b) * a.Hkv + h;
-  uint4 lo[2], hi[2];
-  if (v < a.kept) {
-    int slot = static_cast<int>(v);
-    if (v >= a.sink) {
-      slot = a.ring0[b] + static_cast<int>(v) - a.sink;
-      if (slot >= a.window) slot -= a.window;
-      slot += a.sink;
-    }
-    const int page = checked_page(a.table[static_cast<int64_t>(b) * a.stride + (slot >> a.page_shift)], a.num_pages);
-    const int64_t unit = (page < 0 ? 0 : page) * static_cast<int64_t>(a.Hkv) + h;
-    const int64_t at = ((unit << a.page_shift) + (slot & ((1 << a.page_shift) - 1))) * per_row + c;
-    if (page < 0) atomicCAS(a.error_word, 0u, kPageError);
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      lo[x] = hi[x] = make_uint4(0, 0, 0, 0);
-      if (page >= 0) dequant16(*(reinterpret_cast<const uint4*>(a.pool[x]) + at), a.scale[x][unit], lo[x], hi[x]);
-    }
-  } else {
-    const int64_t from = ((bh * a.T + (v - a.kept)) * per_row + c) * 2;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      lo[x] = *(reinterpret_cast<const uint4*>(a.chunk[x]) + from);
-      hi[x] = *(reinterpret_cast<const uint4*>(a.chunk[x]) + from + 1);
-    }
-  }
-  const int64_t to = ((bh * L + v) * per_row + c) * 2;
-#pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    reinterpret_cast<uint4*>(a.lin[x])[to] = lo[x];
-    reinterpret_cast<uint4*>(a.lin[x])[to + 1] = hi[x];
-  }
-}
-
-lg_status launch_paged_linearise(const PagedLinearise& a, int B, cudaStream_t stream) {
-  const int64_t blocks = (static_cast<int64_t>(a.kept + a.T) * (a.D / 16) + kGatherThreads - 1) / kGatherThreads;
-  if (blocks > 0x7fffffff || a.Hkv > 65535 || B > kLineariseSeqs) return LG_ERR_UNSUPPORTED;
-  return launch_kernel(true, paged_linearise_kernel, dim3(static_cast<unsigned>(blocks), a.Hkv, B), kGatherThreads, 0, stream, a) == cudaSuccess
-             ? LG_OK : LG_ERR_CUDA;
 }
 
 // ---- single-token attention ---------------------------------------------------------------------
