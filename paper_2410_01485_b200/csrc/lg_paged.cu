@@ -368,23 +368,25 @@ struct GatherArgs {
   const float* scale[2];
   const int64_t* slot_map;   // [B, T]
   uint4* out[2];             // [B, Hkv, T, D]
-  int Hkv, T, D, page_shift, num_pages;
+  int Hkv, T, page_shift, num_pages;
 };
 
+// A thread takes 16 elements of a token's K, then of its V: the slot, then scale and codes, then two 16-byte pieces of the row.  HBM-bound: 3
+// bytes an element, two thirds of them written (32K tokens of 32 heads 126 us, 805 MB at 6.4 TB/s; with K and V or several tokens side by
+// side in a thread 139-145 us: what the thread has in flight is not what counts, and the rows are then written further apart).
+template <int D>
 __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const GatherArgs a) {
   pdl_trigger();
-  const int per_row = a.D / 16;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kGatherThreads + threadIdx.x;
-  const int64_t t = i / per_row;
-  const int c = static_cast<int>(i - t * per_row), h = blockIdx.y, b = blockIdx.z;
+  constexpr int kPerRow = D / 16;
+  const int t = blockIdx.x * (kGatherThreads / kPerRow) + threadIdx.x / kPerRow, c = threadIdx.x % kPerRow, h = blockIdx.y, b = blockIdx.z;
   if (t >= a.T) return;
   pdl_wait();
   const int64_t slot = a.slot_map[static_cast<int64_t>(b) * a.T + t];
   const int64_t page = slot >> a.page_shift;
   const bool on = slot >= 0 && page < a.num_pages;
   const int64_t unit = on ? page * a.Hkv + h : 0;
-  const int64_t at = ((unit << a.page_shift) + (slot & ((1 << a.page_shift) - 1))) * per_row + c;
-  const int64_t to = ((static_cast<int64_t>(b) * a.Hkv + h) * a.T + t) * per_row + c;
+  const int64_t at = ((unit << a.page_shift) + (slot & ((1 << a.page_shift) - 1))) * kPerRow + c;
+  const int64_t to = ((static_cast<int64_t>(b) * a.Hkv + h) * a.T + t) * kPerRow + c;
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
@@ -1278,15 +1280,15 @@ lg_status lg_paged_gather(const lg_paged_params* p, const void* k_pool, const vo
   if (T == 0) return LG_OK;
   if (bad_pools(k_pool, v_pool, k_scale, v_scale) || !slot_map || !k_out || !v_out) return LG_ERR_INVALID_ARG;
   if (!aligned(slot_map, 8) || !aligned16(k_out) || !aligned16(v_out)) return LG_ERR_INVALID_ARG;
-  const int64_t blocks = (static_cast<int64_t>(T) * (p->D / 16) + kGatherThreads - 1) / kGatherThreads;
-  if (blocks > 0x7fffffff || p->Hkv > 65535 || p->B > 65535) return LG_ERR_UNSUPPORTED;
+  const int rows = kGatherThreads / (p->D / 16);   // tokens of a block
+  if (T > (1 << 30) || p->Hkv > 65535 || p->B > 65535) return LG_ERR_UNSUPPORTED;
   if ((s = check_arch()) != LG_OK) return s;
   GatherArgs a;
   a.pool[0] = static_cast<const uint8_t*>(k_pool); a.pool[1] = static_cast<const uint8_t*>(v_pool);
   a.scale[0] = k_scale; a.scale[1] = v_scale; a.slot_map = slot_map;
   a.out[0] = static_cast<uint4*>(k_out); a.out[1] = static_cast<uint4*>(v_out);
-  a.Hkv = p->Hkv; a.T = T; a.D = p->D; a.page_shift = page_shift(p->page_tokens); a.num_pages = p->num_pages;
-  return launch_kernel(true, paged_gather_kernel, dim3(static_cast<unsigned>(blocks), p->Hkv, p->B), kGatherThreads, 0,
+  a.Hkv = p->Hkv; a.T = T; a.page_shift = page_shift(p->page_tokens); a.num_pages = p->num_pages;
+  return launch_kernel(true, p->D == 128 ? paged_gather_kernel<128> : paged_gather_kernel<64>, dim3((T + rows - 1) / rows, p->Hkv, p->B), kGatherThreads, 0,
                        static_cast<cudaStream_t>(stream), a) == cudaSuccess ? LG_OK : LG_ERR_CUDA;
 }
 

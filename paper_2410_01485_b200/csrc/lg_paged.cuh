@@ -50,9 +50,9 @@ struct PagedLinearise {
   int ring0[kLineariseSeqs]; // ring offset of each sequence's oldest kept token
 };
 __device__ __forceinline__ void paged_linearise(const PagedLinearise& a, int64_t i, int h, int b) {
-  const int per_row = a.D / 16, L = a.kept + a.T;
-  const int64_t v = i / per_row;
-  const int c = static_cast<int>(i - v * per_row);
+  const int row_shift = a.D == 128 ? 3 : 2, per_row = 1 << row_shift, L = a.kept + a.T;
+  const int64_t v = i >> row_shift;
+  const int c = static_cast<int>(i) & (per_row - 1);
   if (v >= L) return;
   const int64_t bh = static_cast<int64_t>(b) * a.Hkv + h;
   uint4 lo[2], hi[2];
