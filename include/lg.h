@@ -366,7 +366,8 @@ lg_status lg_sparse_decode_static_reset(void* stream);
  *                      should be: lg_paged_append drops the token, lg_paged_slot_map answers -1, lg_paged_decode
  *                      does not attend it, and lg_paged_chunk_prefill writes no result; the last two report
  *                      LG_ERR_PAGE through lg_last_status() on their workspace.
- * Several sequences may read the same page; a page that is appended to must belong to one sequence only.
+ * Several sequences may read the same page; a page that is appended to must belong to one sequence only, once, and
+ * k_pool / v_pool (k_scale / v_scale) must be two arrays there.
  * Counts (n_tokens) are 64-bit; a negative one addresses nothing.
  */
 typedef struct {
@@ -435,8 +436,9 @@ lg_status lg_paged_decode(const lg_paged_params* p, const void* q, const void* k
  * lg_paged_append).  n_tokens_before: HOST int64 [B], >= 0 each; neighbouring sequences that keep the same number of
  * tokens are worked together.  sink_tokens and window_tokens are multiples of 64, window_tokens >= 64.  The cache is
  * copied in bf16 and in time order into the workspace (device, 256-byte aligned,
- * lg_paged_chunk_prefill_workspace_bytes() bytes), and the forward kernel runs over it.  A failure of any of the
- * launches is reported by lg_last_status(workspace, stream).                                                         */
+ * lg_paged_chunk_prefill_workspace_bytes() bytes), and the forward kernel runs over it.  As there, a V that is not finite
+ * reaches every query whose tile holds its token, whether the query sees it or not (tokens that no query of the chunk sees
+ * are left out).  A failure of any of the launches is reported by lg_last_status(workspace, stream).                                                         */
 size_t lg_paged_chunk_prefill_workspace_bytes(const lg_paged_params* p, int32_t T, const int64_t* n_tokens_before);
 lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, const void* k_chunk,
                                  const void* v_chunk, const void* k_pool, const void* v_pool, const float* k_scale,

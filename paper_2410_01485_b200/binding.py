@@ -449,6 +449,14 @@ def _check_cache(p: PagedParams, k_pool, v_pool, k_scale, v_scale):
         "expect pools [num_pages, Hkv, page_tokens, D] and scales [num_pages, Hkv]"
     assert k_pool.is_contiguous() and v_pool.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()
     assert (code is _F8 or code is _U8) and v_pool.dtype is code and k_scale.dtype is _F32 and v_scale.dtype is _F32
+    _check_device(k_pool, v_pool, k_scale, v_scale)
+
+
+def _check_device(*tensors):
+    """All of a call's tensors lie on the device whose stream it goes to (a host tensor's address would fault the GPU)."""
+    dev = _device() if _raw_stream is not None else torch.cuda.current_device()
+    for t in tensors:
+        assert t.get_device() == dev, "expect tensors on the current CUDA device"
 
 
 def _check_table(p: PagedParams, block_table):
@@ -479,6 +487,7 @@ def lg_paged_table_extend(p: PagedParams, n_tokens_before, n_new, free_pages, fr
         assert T_new is not None
     _check_table(p, block_table)
     assert free_pages.dtype is _I32 and free_start.dtype is _I32 and free_next.dtype is _I32 and free_pages.is_contiguous()
+    _check_device(n_tokens_before, block_table, free_pages, free_start, free_next, n_new if n_new is not None else free_next)
     code = load_library().lg_paged_table_extend(
         C.byref(p), n_tokens_before.data_ptr(), _ptr(n_new), 0x7fffffff if T_new is None else T_new, free_pages.data_ptr(),
         free_pages.numel(), free_start.data_ptr(), block_table.data_ptr(), free_next.data_ptr(), _stream())
@@ -495,6 +504,7 @@ def lg_paged_slot_map(p: PagedParams, n_tokens, first, count, block_table, slot_
         _check_counts(B, _I32, count)
     _check_table(p, block_table)
     assert B == p.B and slot_map.dtype is _I64 and slot_map.is_contiguous()
+    _check_device(n_tokens, first, block_table, slot_map, count if count is not None else first)
     code = load_library().lg_paged_slot_map(C.byref(p), n_tokens.data_ptr(), first.data_ptr(), _ptr(count), T, block_table.data_ptr(),
                                             slot_map.data_ptr(), _stream())
     if code != LG_OK:
@@ -510,6 +520,7 @@ def _append_args(p: PagedParams, k_pool, v_pool, k_scale, v_scale, block_table, 
     if n_new is not None:
         _check_counts(B, _I32, n_new)
     assert B == p.B and H == p.Hkv and D == p.D and v_new.shape == shape and k_new.dtype is _BF16 and v_new.dtype is _BF16
+    _check_device(block_table, k_new, v_new, n_tokens_before, n_new if n_new is not None else n_tokens_before)
     if k_new.is_contiguous() and v_new.is_contiguous():
         st = None
     else:
@@ -551,6 +562,7 @@ def lg_paged_gather(p: PagedParams, k_pool, v_pool, k_scale, v_scale, slot_map, 
         v_out = torch.empty_like(k_out)
     for t in (k_out, v_out):
         assert t.shape == shape and t.dtype is _BF16 and t.is_contiguous()
+    _check_device(slot_map, k_out, v_out)
     _check(load_library().lg_paged_gather(C.byref(p), k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
                                           slot_map.data_ptr(), T, k_out.data_ptr(), v_out.data_ptr(), _stream()), "lg_paged_gather")
     return k_out, v_out
@@ -575,6 +587,7 @@ def _decode_args(p: PagedParams, q, k_pool, v_pool, k_scale, v_scale, block_tabl
     for t in (q, o):
         assert t.shape == shape and t.dtype is _BF16 and t.is_contiguous()
     assert lse is None or (lse.shape == shape[:2] and lse.dtype is _F32 and lse.is_contiguous())
+    _check_device(q, block_table, n_tokens, o, workspace, lse if lse is not None else o)
     return (C.byref(p), q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
             block_table.data_ptr(), n_tokens.data_ptr(), o.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel())
 
@@ -585,7 +598,7 @@ def lg_paged_decode(p: PagedParams, q, k_pool, v_pool, k_scale, v_scale, block_t
     o = torch.empty_like(q) if o is None else o
     if lse is None and want_lse:
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-    ws = paged_decode_workspace(p, q.device) if workspace is None else workspace
+    ws = paged_decode_workspace(p) if workspace is None else workspace
     _check(load_library().lg_paged_decode(*_decode_args(p, q, k_pool, v_pool, k_scale, v_scale, block_table, n_tokens, o, lse, ws),
                                           _stream()), "lg_paged_decode")
     return o, lse
@@ -634,9 +647,13 @@ def lg_paged_chunk_prefill(p: PagedParams, q_chunk, k_chunk, v_chunk, k_pool, v_
     B, T, D = p.B, q_chunk.shape[2], p.D
     for t, H in ((q_chunk, p.Hq), (k_chunk, p.Hkv), (v_chunk, p.Hkv)):
         assert t.shape == (B, H, T, D) and t.dtype is _BF16 and t.is_contiguous()
+    _check_device(q_chunk, k_chunk, v_chunk, block_table)
     o = torch.empty_like(q_chunk) if o is None else o
     lse = torch.empty(q_chunk.shape[:3], dtype=torch.float32, device=q_chunk.device) if lse is None else lse
-    ws = paged_chunk_prefill_workspace(p, T, n_tokens_before, q_chunk.device) if workspace is None else workspace
+    ws = paged_chunk_prefill_workspace(p, T, n_tokens_before) if workspace is None else workspace
+    assert o.shape == q_chunk.shape and o.dtype is _BF16 and o.is_contiguous()
+    assert lse.shape == q_chunk.shape[:3] and lse.dtype is _F32 and lse.is_contiguous()
+    _check_device(o, lse, ws)
     _check(load_library().lg_paged_chunk_prefill(
         C.byref(p), q_chunk.data_ptr(), k_chunk.data_ptr(), v_chunk.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
         k_scale.data_ptr(), v_scale.data_ptr(), block_table.data_ptr(), T, _host_counts(p, n_tokens_before), o.data_ptr(),

@@ -749,6 +749,14 @@ lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, 
     l.pool[0] = k_pool; l.pool[1] = v_pool; l.scale[0] = k_scale; l.scale[1] = v_scale;
     l.error_word = reinterpret_cast<unsigned int*>(ws);
     l.Hkv = p->Hkv; l.D = p->D; l.T = T; l.kept = c.kept; l.sink = p->sink_tokens; l.window = p->window_tokens;
+    // the chunk's first token sees the furthest back: behind the sink the rows v with (kept + phase) / block - (v + phase) / block < window / block
+    l.hidden = 0;
+    if (p->block_tokens > 0) {
+      const int first = ((c.kept + c.r.win_phase) / p->block_tokens - p->window_tokens / p->block_tokens + 1) * p->block_tokens - c.r.win_phase;
+      l.hidden = first < 0 ? 0 : first;
+    } else if (c.kept == p->sink_tokens + p->window_tokens) {
+      l.hidden = p->sink_tokens + 1;   // (a full ring: its oldest token has left the window)
+    }
     l.page_shift = page_shift(p->page_tokens); l.num_pages = p->num_pages; l.stride = stride;
     __nv_bfloat16* lin[2] = {reinterpret_cast<__nv_bfloat16*>(ws + c.o_k), reinterpret_cast<__nv_bfloat16*>(ws + c.o_v)};
     for (int x = b; x < e; x += kLineariseSeqs) {

@@ -548,8 +548,8 @@ static __device__ __noinline__ int2 left_out(int64_t n, int C, int sink, int blo
   return make_int2(static_cast<int>((first_held - sink) % w), static_cast<int>(first_kept - first_held));
 }
 
-// Two neighbouring results of a row, and its LSE.
-__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + fast_log2(l)) * 0.6931471805599453f : -INFINITY; }
+// (A sum of zero: nothing was attended.  One that is NaN stays NaN.)
+__device__ __forceinline__ float lse_of(float m, float l) { return l != 0.f ? (m + fast_log2(l)) * 0.6931471805599453f : -INFINITY; }
 
 // The records of a unit, one per CTA from first_cta on, merged in that order into o and lse: a warp per head, a lane per record's weight.
 // The records sit in the L2, a round trip of a microsecond away: the values of up to 32 travel together, and their weights with them.
@@ -599,10 +599,10 @@ __device__ __forceinline__ void merge_records(const PagedDecodeArgs& a, int64_t 
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-  const float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
+  const float inv = l != 0.f ? __fdividef(1.f, l) : 0.f;
 #pragma unroll
   for (int z = 0; z < V; z += 2)
-    reinterpret_cast<uint32_t*>(a.o + (qh0 + head) * D + lane * V)[z / 2] = l > 0.f ? pack_bf16(acc[z] * inv, acc[z + 1] * inv) : 0u;
+    reinterpret_cast<uint32_t*>(a.o + (qh0 + head) * D + lane * V)[z / 2] = l != 0.f ? pack_bf16(acc[z] * inv, acc[z + 1] * inv) : 0u;
   if (lane == 0 && a.lse) a.lse[qh0 + head] = lse_of(m, l);
 }
 
@@ -983,7 +983,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
           const int gh = cur.hg * kDecHeads + 2 * c + x;
           if (gh >= a.G) continue;
           const int64_t qh = static_cast<int64_t>(cur.b) * a.Hq + cur.kvh * a.G + gh;
-          const float f = l_run[x] > 0.f ? g[x] * __fdividef(1.f, l_run[x]) : 0.f;
+          const float f = l_run[x] != 0.f ? g[x] * __fdividef(1.f, l_run[x]) : 0.f;
           uint32_t* to = reinterpret_cast<uint32_t*>(a.o + qh * D) + r;
 #pragma unroll
           for (int y = 0; y < D / 16; ++y) to[8 * y] = pack_bf16(oacc[y][x] * f, oacc[y][2 + x] * f);
@@ -1047,10 +1047,10 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
     const int gh = __shfl_sync(0xffffffffu, mine_of.w, y0) * kDecHeads + warp;
     if (gh >= a.G) continue;
     const int64_t qh = static_cast<int64_t>(b) * a.Hq + kvh * a.G + gh;
-    const float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
+    const float inv = l != 0.f ? __fdividef(1.f, l) : 0.f;
 #pragma unroll
     for (int x = 0; x < D / 32; x += 2)
-      *reinterpret_cast<uint32_t*>(a.o + qh * D + lane * 2 + 32 * x) = l > 0.f ? pack_bf16(acc[x] * inv, acc[x + 1] * inv) : 0u;
+      *reinterpret_cast<uint32_t*>(a.o + qh * D + lane * 2 + 32 * x) = l != 0.f ? pack_bf16(acc[x] * inv, acc[x + 1] * inv) : 0u;
     if (lane == 0 && a.lse) a.lse[qh] = lse_of(m, l);
   }
 
@@ -1224,6 +1224,7 @@ lg_status lg_paged_append(const lg_paged_params* p, void* k_pool, void* v_pool, 
   if (bad_pools(k_pool, v_pool, k_scale, v_scale) || !block_table || !k_new || !v_new || !n_tokens_before) return LG_ERR_INVALID_ARG;
   if (!aligned(block_table, 4) || !aligned16(k_new) || !aligned16(v_new) || !aligned(n_tokens_before, 8) || !aligned(n_new, 4))
     return LG_ERR_INVALID_ARG;
+  if (k_pool == v_pool || k_scale == v_scale) return LG_ERR_INVALID_ARG;   // K and V are written side by side
   AppendArgs a;
   a.stride_t = p->D;
   a.stride_h = static_cast<int64_t>(T_new) * p->D;

@@ -37,7 +37,8 @@ constexpr int kGatherThreads = 256;
 
 // What a chunk attends to, as one sequence in time order: the `kept` tokens that the cache holds (the sink, then the ring from its
 // oldest token on, ring0 of the sequence), then the chunk's own rows.  One thread: 16 elements of K and of V, piece i of kv head h of
-// sequence b.  Rows whose page is absent are zeros.
+// sequence b.  Rows whose page is absent are zeros, and so are those [sink, hidden) that no token of the chunk sees (a window edge that is
+// block-aligned): the weight of zero that they get does not silence a NaN.
 constexpr int kLineariseSeqs = 128;   // sequences of one launch
 struct PagedLinearise {
   const void* pool[2];       // K, V
@@ -46,7 +47,7 @@ struct PagedLinearise {
   void* lin[2];              // [B, Hkv, kept + T, D] bf16
   const int32_t* table;
   unsigned int* error_word;
-  int B, Hkv, D, T, kept, sink, window, page_shift, num_pages, stride;
+  int B, Hkv, D, T, kept, sink, hidden, window, page_shift, num_pages, stride;
   int ring0[kLineariseSeqs]; // ring offset of each sequence's oldest kept token
 };
 __device__ __forceinline__ void paged_linearise(const PagedLinearise& a, int64_t i, int h, int b) {
@@ -63,7 +64,8 @@ __device__ __forceinline__ void paged_linearise(const PagedLinearise& a, int64_t
       if (slot >= a.window) slot -= a.window;
       slot += a.sink;
     }
-    const int page = checked_page(a.table[static_cast<int64_t>(b) * a.stride + (slot >> a.page_shift)], a.num_pages);
+    int page = checked_page(a.table[static_cast<int64_t>(b) * a.stride + (slot >> a.page_shift)], a.num_pages);
+    if (v >= a.sink && v < a.hidden) page = -1;
     const int64_t unit = (page < 0 ? 0 : page) * static_cast<int64_t>(a.Hkv) + h;
     const int64_t at = ((unit << a.page_shift) + (slot & ((1 << a.page_shift) - 1))) * per_row + c;
 #pragma unroll

@@ -176,6 +176,8 @@ APPENDS = [  # n, T, new, Hkv, D, sink, window, P
     ([17, 1 << 40], 1000, [999, 1000], 1, 64, 0, 333, 128),
     ([0, 90], 777, None, 1, 128, 10, 300, 128),
     ([200, -1, 10], 2, [2, 2, -4], 2, 64, 0, 96, 64),
+    ([200, -1, 10, 0, 1 << 40], 1, [1, 1, 0, 3, 1], 2, 128, 5, 203, 128),
+    ([7, 0, 63, 64, 100], 1, [0, 1, 1, -2, 1], 3, 64, 0, 64, 16),
 ]
 
 
@@ -217,14 +219,15 @@ def test_append_grows_and_shrinks_scales(lg):
         s.same_state()
 
 
-def test_append_bad_pages_and_neighbours(lg):
+@pytest.mark.parametrize("T", [1, 40])
+def test_append_bad_pages_and_neighbours(lg, T):
     """Table entries that name no page: their tokens are dropped, nothing else is touched."""
-    s = Setup(lg, [60, 3, 90], 2, 2, 128, 0, 96, 32)
+    s = Setup(lg, [64, 3, 90], 2, 2, 128, 0, 96, 32)
     s.ref.table[0, 2] = -1
     s.ref.table[1, 0] = s.num_pages
     s.ref.table[2, :] = np.iinfo(np.int32).max
     s.upload()
-    k, v = randn(3, 2, 40, 128, seed=1), randn(3, 2, 40, 128, seed=2)
+    k, v = randn(3, 2, T, 128, seed=1), randn(3, 2, T, 128, seed=2)
     lg.lg_paged_append(s.p, *s.cache, s.table, k, v, s.counts())
     for b in range(3):
         s.ref.append(b, s.n[b], np64(k)[b], np64(v)[b])
@@ -343,6 +346,30 @@ def test_decode_absent_pages_are_reported_and_left_out(lg):
     assert torch.isinf(lse[2]).all() and not o[2].any()
 
 
+@pytest.mark.parametrize("where", ["k", "v", "q"])
+def test_decode_nan_that_is_attended_stays(lg, where):
+    """... in the heads that read it, and only there; in a run of its own, a shared unit and a CTA's piece."""
+    s = Setup(lg, [2000, 40, 33], 4, 2, 128, 0, 2048, 16)
+    q = randn(3, 4, 128, seed=5)
+    clean = lg.lg_paged_decode(s.p, q, *s.cache, s.table, s.counts())
+    for b in range(3):
+        if where == "q":
+            q[b, 2, 5] = float("nan")
+        else:
+            s.ref.codes[where == "v"][s.ref.page(b, 30), 1, 30 % 16, 7] = 127
+    s.upload()
+    o, lse = lg.lg_paged_decode(s.p, q, *s.cache, s.table, s.counts())
+    hit = torch.zeros(4, dtype=torch.bool, device="cuda")
+    hit[2:3 if where == "q" else 4] = True
+    assert torch.equal(o[:, ~hit], clean[0][:, ~hit]) and torch.equal(lse[:, ~hit], clean[1][:, ~hit])
+    if where == "v":
+        assert torch.isnan(o[:, hit, 7]).all() and torch.equal(lse, clean[1])
+        o[:, hit, 7] = clean[0][:, hit, 7]
+        assert torch.equal(o, clean[0])
+    else:
+        assert torch.isnan(o[:, hit]).all() and torch.isnan(lse[:, hit]).all()
+
+
 def test_decode_shared_pages_and_scale(lg):
     """Two sequences read the same pages (a shared prompt); a softmax scale of one's own."""
     s = Setup(lg, [90, 200, 90], 4, 2, 64, 0, 256, 16)
@@ -430,6 +457,79 @@ def test_chunk(lg, case):
                     assert np.all(np.abs(od[b, g, t] - want) <= tol) and abs(ld[b, g, t] - l) <= tol_l, (b, g, t)
     again = lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n, workspace=ws)
     assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
+
+
+def _check_chunk_rows(s, n, T, q, k, v, o, lse, rows, heads, weight=2.0 ** -8):
+    p, c = s.p, s.ref
+    G = p.Hq // p.Hkv
+    for b in range(len(n)):
+        for g in heads:
+            h = g // G
+            pos, ck, cv = c.rows(b, h, n[b])
+            pos = np.concatenate([pos, np.arange(n[b], n[b] + T)])
+            ck, cv = np.concatenate([ck, np64(k[b, h])]), np.concatenate([cv, np64(v[b, h])])
+            for t in rows:
+                see = R.visible(n[b] + t, pos, c.sink, c.window, s.block)
+                want, l, tol, tol_l = R.attend(np64(q[b, g, t]), ck, cv, see, 1 / math.sqrt(p.D), weight)
+                assert np.all(np.abs(np64(o[b, g, t]) - want) <= tol) and abs(lse[b, g, t].item() - l) <= tol_l, (b, g, t)
+
+
+def test_chunk_of_more_rows_than_one_block_schedules(lg):
+    T, n = 17000, [90]                                            # 67 super-tiles
+    s = Setup(lg, n, 2, 1, 64, 0, 128, 64)
+    q, k, v = randn(1, 2, T, 64, seed=1), randn(1, 1, T, 64, seed=2), randn(1, 1, T, 64, seed=3)
+    ws = lg.paged_chunk_prefill_workspace(s.p, T, n)
+    o, lse = lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n, workspace=ws)
+    assert lg.lg_last_status(ws) == 0
+    _check_chunk_rows(s, n, T, q, k, v, o, lse, [0, 1, 37, 38, 255, 256, 9999, 16639, 16640, T - 1], [0, 1])
+
+
+def test_chunk_of_more_sequences_than_one_launch(lg):
+    B, T = 133, 3
+    n = [70 + b for b in range(B)]                                # full rings: one run of neighbours, each at its own offset
+    n[131] = 5
+    s = Setup(lg, n, 1, 1, 64, 0, 64, 16)
+    q, k, v = randn(B, 1, T, 64, seed=1), randn(B, 1, T, 64, seed=2), randn(B, 1, T, 64, seed=3)
+    ws = lg.paged_chunk_prefill_workspace(s.p, T, n)
+    o, lse = lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n, workspace=ws)
+    assert lg.lg_last_status(ws) == 0
+    _check_chunk_rows(s, n, T, q, k, v, o, lse, range(T), [0])
+    s.ref.table[130, 2] = -1                                      # found by the launch that starts behind the first 128
+    s.upload()
+    lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n, workspace=ws)
+    assert lg.lg_last_status(ws) == -7
+
+
+@pytest.mark.parametrize("D, Hq", [(128, 4), (64, 2)])
+def test_chunk_over_keys_that_raise_the_maximum(lg, D, Hq):
+    """Tokens far above the ones before them, again and again: references that move late, by a lot, and not at all."""
+    n, T = [400], 300
+    s = Setup(lg, n, Hq, 1, D, 64, 256, 32, scales=(0, 0))
+    q, k, v = randn(1, Hq, T, D, seed=1), randn(1, 1, T, D, seed=2), randn(1, 1, T, D, seed=3)
+    big = torch.ones(T, 1, device="cuda")
+    big[torch.arange(0, T, 37)] = 6.0
+    big[150], big[200] = 20.0, 40.0                               # scores in the hundreds: past 2^40 of what came before
+    k = (k.float() * big).to(torch.bfloat16)
+    o, lse = lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n)
+    _check_chunk_rows(s, n, T, q, k, v, o, lse, range(0, T, 7), range(Hq))
+
+
+@pytest.mark.parametrize("block", [0, 64])
+def test_chunk_reads_nothing_that_no_row_sees(lg, block):
+    """NaN in the ring's tokens that have left the window of the chunk's first row, in stale pages and empty slots."""
+    n, T = [400, 1000, 120], 40
+    s = Setup(lg, n, 2, 1, 64, 64, 128, 32, block=block)
+    q, k, v = randn(3, 2, T, 64, seed=1), randn(3, 1, T, 64, seed=2), randn(3, 1, T, 64, seed=3)
+    clean = lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n)
+    used = {(s.ref.page(b, slot), slot % 32) for b in range(3) for slot, j in R.ring(n[b], 64, 128).items()
+            if any(R.visible(n[b] + t, np.array([j]), 64, 128, block)[0] for t in range(T))}
+    for page in range(s.num_pages):
+        for off in range(32):
+            if (page, off) not in used:
+                s.ref.codes[0][page, :, off] = s.ref.codes[1][page, :, off] = 127
+    s.upload()
+    o, lse = lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n)
+    assert torch.equal(o, clean[0]) and torch.equal(lse, clean[1])
 
 
 def test_chunk_absent_page_is_reported_and_writes_nothing(lg):
@@ -545,6 +645,22 @@ def test_two_streams_with_a_workspace_each(lg):
     torch.cuda.synchronize()
     for (o, lse), (wo, wl) in zip(outs, want):
         assert torch.equal(o, wo) and torch.equal(lse, wl)
+
+
+def test_tensors_of_the_host_are_refused(lg):
+    s = Setup(lg, [40], 2, 1, 64, 0, 64, 16)
+    q, n = randn(1, 2, 64, seed=1), s.counts()
+    for bad in ("q", "n", "table", "scale"):
+        args = dict(q=q, n=n, table=s.table, scale=s.scales[0])
+        args[bad] = args[bad].cpu()
+        with pytest.raises(AssertionError):
+            lg.lg_paged_decode(s.p, args["q"], *s.pools, args["scale"], s.scales[1], args["table"], args["n"], o=torch.empty_like(q))
+    for wrong in (s.counts().int(), s.counts([1, 2])):
+        with pytest.raises(AssertionError):
+            lg.lg_paged_decode(s.p, q, *s.cache, s.table, wrong)
+    k = randn(1, 1, 1, 64)
+    with pytest.raises(lg.LgError):                               # one array for K and V
+        lg.lg_paged_append(s.p, s.pools[0], s.pools[0], *s.scales, s.table, k, k, n)
 
 
 def test_marshalled_calls(lg):

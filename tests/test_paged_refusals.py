@@ -26,7 +26,7 @@ def _calls(lib, p, **kw):
     n = (C.c_int64 * 4)(10, 10, 10, 10)
     args = {"lg_paged_table_extend": dict(n=256, new=256, T=4, free=256, n_free=9, start=256, table=256, next=512, stream=None),
             "lg_paged_slot_map": dict(n=256, first=256, count=256, T=4, table=256, map=256, stream=None),
-            "lg_paged_append": dict(k=256, v=256, ks=256, vs=256, table=256, kn=256, vn=256, strides=None, T=4, n=256, new=256, stream=None),
+            "lg_paged_append": dict(k=256, v=512, ks=256, vs=512, table=256, kn=256, vn=256, strides=None, T=4, n=256, new=256, stream=None),
             "lg_paged_gather": dict(k=256, v=256, ks=256, vs=256, map=256, T=4, ko=256, vo=256, stream=None),
             "lg_paged_decode": dict(q=256, k=256, v=256, ks=256, vs=256, table=256, n=256, o=256, lse=256, ws=256, bytes=big, stream=None),
             "lg_paged_chunk_prefill": dict(q=256, kn=256, vn=256, k=256, v=256, ks=256, vs=256, table=256, T=4, hn=n, o=256, lse=256,
@@ -122,3 +122,7 @@ def test_sizes_beyond_what_is_covered(lib):
     long = _good(B=1, Hq=256, Hkv=256, window_tokens=(1 << 30) - 64, num_pages=10)
     assert lib.lg_paged_decode_workspace_bytes(C.byref(long)) == 0
     assert _calls(lib, long)["lg_paged_decode"] == UNSUPPORTED
+
+
+def test_append_writes_two_arrays(lib):
+    assert _calls(lib, _good(), v=256)["lg_paged_append"] == INVALID and _calls(lib, _good(), vs=256)["lg_paged_append"] == INVALID
