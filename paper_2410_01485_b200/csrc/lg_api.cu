@@ -58,7 +58,7 @@ lg_status resolve(const lg_attn_params* p, Resolved* r, bool want_bwd, int kv_to
   r->pat.nB = (p->L + p->block - 1) / p->block;
   r->pat.mode = p->mode;
   r->pat.ns = r->pat.nw = r->pat.stride = r->pat.nl = 0;
-  r->max_prob = 256.f;
+  r->late_reference = false;
   r->pat.doc_start = nullptr;
   r->pat.block = p->block;
   r->exact_w = 0;
@@ -668,10 +668,6 @@ lg_status lg_chunk_prefill(const lg_decode_params* p, const void* q_chunk, const
 // The sequences are taken in runs of neighbours that keep as many tokens (and, with a block-aligned window, have the same phase): the
 // attention kernel's rows are counted from the number of kept tokens.  Rings that are full, and a batch at one position, are one run.
 namespace {
-// The keys of real caches are not N(0,1): channels of unequal size and single tokens far above the rest raise a row's maximum again and
-// again, and each time the warp works its half tile twice and rescales its rows.  fp32 sums and bf16 probabilities hold 2^40 as well as
-// 2^8 (all that changes is where log2 of the sum rounds: 2^-19 of 40).  Chunk of 1500 tokens, 64 / 8 heads, such keys: 531 us at 2^8.
-constexpr float kChunkMaxProb = 1.0995e12f;
 lg_decode_params ring_of(const lg_paged_params* p, int B) {
   lg_decode_params d;
   d.B = B; d.Hq = p->Hq; d.Hkv = p->Hkv; d.D = p->D;
@@ -735,7 +731,7 @@ lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, 
     const lg_decode_params d = ring_of(p, e - b);
     ChunkPlan c;
     if ((s = plan_chunk(&d, T, n, &c)) != LG_OK) return s;
-    c.r.max_prob = kChunkMaxProb;
+    c.r.late_reference = true;
     const bool one = c.r.n_stiles <= kChunkMaxTiles;
     if (!one && (s = prepare_workspace(c.r, c.w, ws, 1, true, 0, st)) != LG_OK) return s;
     SchedArgs sched{};

@@ -4,7 +4,7 @@
 
 namespace lg {
 
-template <int D, int BS, int NB, bool kSplit>
+template <int D, int BS, int NB, bool kSplit, bool kRefine = false>
 static lg_status launch_fwd_t(const Resolved& r, const WsLayout& w, const void* q, const void* k, const void* v,
                               void* o, float* lse, uint8_t* ws, cudaStream_t stream) {
   CUtensorMap tq, tk, tv;
@@ -29,10 +29,10 @@ static lg_status launch_fwd_t(const Resolved& r, const WsLayout& w, const void* 
   a.win_block = r.win_block; a.win_phase = r.win_phase;
   a.doc_start = r.doc_start;
   a.scale_log2 = r.scale * 1.4426950408889634f;
-  a.max_prob = r.max_prob;
+  a.max_prob = kRefine ? kFwdLateProb : kFwdMaxProb;
   a.head_group = head_group(r, r.B * r.Hq);
   a.split = r.fsplit;
-  auto kern = fwd_kernel<D, BS, NB, kSplit>;
+  auto kern = fwd_kernel<D, BS, NB, kSplit, kRefine>;
   constexpr int smem = FwdSmem<D>::kTotal;
   static std::atomic<bool> allowed[kMaxDevices];
   // cut tiles: clusters of as many CTAs as a tile has places; the last cluster is filled up
@@ -46,6 +46,10 @@ lg_status launch_fwd(const Resolved& r, const WsLayout& w, const void* q, const 
                      float* lse, uint8_t* ws, cudaStream_t stream) {
   if (r.n_qtiles > 65535) return LG_ERR_UNSUPPORTED;
   const bool pairs = fwd_two_ctas(r);
+  if (r.late_reference && r.block == 64 && r.fsplit.len == 0) {
+    if (r.D == 128) return launch_fwd_t<128, 64, 2, false, true>(r, w, q, k, v, o, lse, ws, stream);
+    return pairs ? launch_fwd_t<64, 64, 1, false, true>(r, w, q, k, v, o, lse, ws, stream) : launch_fwd_t<64, 64, 2, false, true>(r, w, q, k, v, o, lse, ws, stream);
+  }
 #define LG_FWD_CASE(DD, BB, NN) \
   if (r.D == DD && r.block == BB && pairs == (NN == 1)) return launch_fwd_t<DD, BB, NN, false>(r, w, q, k, v, o, lse, ws, stream);
   // (where a part of a device cannot hold a cluster the launch is refused, and the tiles stay whole)

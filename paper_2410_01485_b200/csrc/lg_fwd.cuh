@@ -35,6 +35,12 @@
 
 namespace lg {
 
+constexpr float kFwdMaxProb = 256.0f;   // a half's probabilities may grow to this (relative to the row's reference) before the reference moves
+// ... and to this where the caller expects maxima that rise again and again (a cache's real keys: channels of unequal size, single tokens far
+// above the rest), each of which costs a warp its half tile twice and a rescaling of its rows: fp32 sums and bf16 probabilities hold 2^40 as well
+// as 2^8 (log2 of the sum rounds by 2^-19 of 40).
+constexpr float kFwdLateProb = 1.0995e12f;
+
 struct FwdArgs {
   const int32_t* tile_ent;   // kb * 16 + member mask (bit r: pattern row r of the super-tile has the block)
   const TileRec* order;      // [n_super_tiles] by launch rank
@@ -143,7 +149,8 @@ __device__ __forceinline__ void fwd_join(const FwdArgs& a, uint32_t base, uint32
   else fwd_join_rows<D, 8, 2>(a, base, n_segs, b, h, row0, first, end, step, c);
 }
 
-template <int D, int BS, int NB /* score buffers per slot */, bool kSplit>
+// kRefine: O is divided by the sum of the probabilities as they were rounded to bf16 where they weigh, the LSE by that of the unrounded ones (below).
+template <int D, int BS, int NB /* score buffers per slot */, bool kSplit, bool kRefine = false>
 __global__ void __launch_bounds__(kFwdThreads, fwd_ctas_per_sm(NB))
 fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
            const __grid_constant__ CUtensorMap tm_v, const FwdArgs a) {
@@ -250,6 +257,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
   // of a softmax thread's row:
   float m_ref = -INFINITY;   // reference maximum (scaled, log2 domain) the probabilities are relative to
   float l_run = 0.f;
+  float c_run = 0.f;         // kRefine: the rounded probabilities' sum less l_run, over the halves where it was looked at
   int p0 = 0, p1 = 0;        // P tiles published per score buffer (barrier phases)
   if (warp == kFwdTmaWarp) {
     // ------------------------------ TMA producer ------------------------------------------
@@ -486,7 +494,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
           const float m_new = fmaxf(m_ref, mx * a.scale_log2);
           const bool raise = look && m_new > m_ref;
           const float alpha = raise ? fast_exp2(m_ref - m_new) : 1.f;   // m_ref = -inf -> 0
-          if (raise) { m_ref = m_new; l_run *= alpha; }
+          if (raise) { m_ref = m_new; l_run *= alpha; if constexpr (kRefine) c_run *= alpha; }
           if (p0 + p1 > 0) {   // O already holds products: wait for them, then rescale my row
             ok = wait_o(13);
             if (!ok) break;
@@ -502,6 +510,22 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
             }
           }
           exp_half((m_ref == -INFINITY) ? 0.f : -m_ref);
+        }
+        if constexpr (kRefine) {
+          // A reference that stays behind the maximum costs nothing in fp32, but the largest probability of a row is then a rounded number
+          // like the others, and where one key has most of the weight its rounding is the row's error.  It cancels when the row is
+          // divided by the rounded probabilities' sum.  Only halves that outweigh all before them are looked at.  (Chunk of 1500 tokens, 64 / 8
+          // heads, uneven keys: O is 1.50e-3 off in the norm at 450 us, of which 1.44e-3 are its own rounding; 2.13e-3 without this,
+          // 1.70e-3 at 524 us with references that move from 2^8 on; with halves of a quarter or a sixteenth of the weight 457 us, 459 us, 1.50e-3.)
+          if (__any_sync(0xffffffffu, psum > l_run)) {
+            float d0 = 0.f, d1 = 0.f, d2 = 0.f, d3 = 0.f;
+#pragma unroll
+            for (int x = 0; x < 32; x += 2) {
+              d0 += __uint_as_float(preg[x] << 16); d1 += __uint_as_float(preg[x] & 0xffff0000u);
+              d2 += __uint_as_float(preg[x + 1] << 16); d3 += __uint_as_float(preg[x + 1] & 0xffff0000u);
+            }
+            c_run += ((d0 + d1) + (d2 + d3)) - psum;
+          }
         }
         l_run += psum;
         tmem_st32(my_s + buf * 64, preg);   // P over the first columns of this half's S
@@ -523,7 +547,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
     if (ok && p0 + p1 > 0 && qi - lane < a.L && qi - lane + 32 > a.q_start) {
       const bool mine = qi < a.L && qi >= a.q_start;
       tc_fence_after();
-      const float inv_l = l_run > 0.f ? 1.f / l_run : 0.f;
+      const float inv_l = l_run > 0.f ? 1.f / (kRefine ? l_run + c_run : l_run) : 0.f;
       // rows leave through the slot's own Q tile (its last S product is done: it precedes the last P V in
       // the issuer's queue), 4 KB per warp, so that the stores cover whole rows (store_acc_64cols)
       uint8_t* stage = sQ + s * kTile + (warp & 3) * 4096;
