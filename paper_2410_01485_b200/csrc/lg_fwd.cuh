@@ -475,49 +475,50 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
         // (an unset reference with every column masked gives zeros and stays unset; NaN compares false
         // and cannot appear: masked scores are -inf, whose exponential is 0)
         const bool look = unset ? (lim > lo) : !(psum <= a.max_prob);
-        if (__any_sync(0xffffffffu, look)) {
-          float mx = -INFINITY;
+        // (kRefine: the halves that outweigh all before them are looked at too, with the same vote)
+        if (__any_sync(0xffffffffu, look || (kRefine && psum > l_run))) {
+          if (!kRefine || __any_sync(0xffffffffu, look)) {
+            float mx = -INFINITY;
 #pragma unroll
-          for (int c0 = 0; c0 < 64; c0 += C) {
-            if (NB == 1) load_cols(c0);
-            float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
+            for (int c0 = 0; c0 < 64; c0 += C) {
+              if (NB == 1) load_cols(c0);
+              float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
 #pragma unroll
-            for (int x = 0; x < C; x += 8) {
-              m0 = max3(m0, __uint_as_float(v[x + 0]), __uint_as_float(v[x + 1]));
-              m1 = max3(m1, __uint_as_float(v[x + 2]), __uint_as_float(v[x + 3]));
-              m2 = max3(m2, __uint_as_float(v[x + 4]), __uint_as_float(v[x + 5]));
-              m3 = max3(m3, __uint_as_float(v[x + 6]), __uint_as_float(v[x + 7]));
+              for (int x = 0; x < C; x += 8) {
+                m0 = max3(m0, __uint_as_float(v[x + 0]), __uint_as_float(v[x + 1]));
+                m1 = max3(m1, __uint_as_float(v[x + 2]), __uint_as_float(v[x + 3]));
+                m2 = max3(m2, __uint_as_float(v[x + 4]), __uint_as_float(v[x + 5]));
+                m3 = max3(m3, __uint_as_float(v[x + 6]), __uint_as_float(v[x + 7]));
+              }
+              mx = max3(mx, fmaxf(m0, m1), fmaxf(m2, m3));
             }
-            mx = max3(mx, fmaxf(m0, m1), fmaxf(m2, m3));
-          }
-          // the rows that asked move their reference to the maximum seen so far (the others keep theirs)
-          const float m_new = fmaxf(m_ref, mx * a.scale_log2);
-          const bool raise = look && m_new > m_ref;
-          const float alpha = raise ? fast_exp2(m_ref - m_new) : 1.f;   // m_ref = -inf -> 0
-          if (raise) { m_ref = m_new; l_run *= alpha; if constexpr (kRefine) c_run *= alpha; }
-          if (p0 + p1 > 0) {   // O already holds products: wait for them, then rescale my row
-            ok = wait_o(13);
-            if (!ok) break;
-            tc_fence_after();
+            // the rows that asked move their reference to the maximum seen so far (the others keep theirs)
+            const float m_new = fmaxf(m_ref, mx * a.scale_log2);
+            const bool raise = look && m_new > m_ref;
+            const float alpha = raise ? fast_exp2(m_ref - m_new) : 1.f;   // m_ref = -inf -> 0
+            if (raise) { m_ref = m_new; l_run *= alpha; if constexpr (kRefine) c_run *= alpha; }
+            if (p0 + p1 > 0) {   // O already holds products: wait for them, then rescale my row
+              ok = wait_o(13);
+              if (!ok) break;
+              tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < D / 16; ++c) {
-              uint32_t oreg[16];
-              tmem_ld16(my_o + c * 16, oreg);
-              tmem_ld_wait();
+              for (int c = 0; c < D / 16; ++c) {
+                uint32_t oreg[16];
+                tmem_ld16(my_o + c * 16, oreg);
+                tmem_ld_wait();
 #pragma unroll
-              for (int x = 0; x < 16; ++x) oreg[x] = __float_as_uint(__uint_as_float(oreg[x]) * alpha);
-              tmem_st16(my_o + c * 16, oreg);
+                for (int x = 0; x < 16; ++x) oreg[x] = __float_as_uint(__uint_as_float(oreg[x]) * alpha);
+                tmem_st16(my_o + c * 16, oreg);
+              }
             }
+            exp_half((m_ref == -INFINITY) ? 0.f : -m_ref);
           }
-          exp_half((m_ref == -INFINITY) ? 0.f : -m_ref);
-        }
-        if constexpr (kRefine) {
-          // A reference that stays behind the maximum costs nothing in fp32, but the largest probability of a row is then a rounded number
-          // like the others, and where one key has most of the weight its rounding is the row's error.  It cancels when the row is
-          // divided by the rounded probabilities' sum.  Only halves that outweigh all before them are looked at.  (Chunk of 1500 tokens, 64 / 8
-          // heads, uneven keys: O is 1.50e-3 off in the norm at 450 us, of which 1.44e-3 are its own rounding; 2.13e-3 without this,
-          // 1.70e-3 at 524 us with references that move from 2^8 on; with halves of a quarter or a sixteenth of the weight 457 us, 459 us, 1.50e-3.)
-          if (__any_sync(0xffffffffu, psum > l_run)) {
+         if constexpr (kRefine) {
+            // A reference that stays behind the maximum costs nothing in fp32, but the largest probability of a row is then a rounded number
+            // like the others, and where one key has most of the weight its rounding is the row's error.  It cancels when the row is
+            // divided by the rounded probabilities' sum.  (Chunk of 1500 tokens, 64 / 8 heads, uneven keys: O is 1.50e-3 off in the norm, of which
+            // 1.44e-3 are its own rounding; 2.13e-3 without this, 1.70e-3 with references that move from 2^8 on; looked at in halves of a
+            // quarter of the weight too, no less.)
             float d0 = 0.f, d1 = 0.f, d2 = 0.f, d3 = 0.f;
 #pragma unroll
             for (int x = 0; x < 32; x += 2) {
