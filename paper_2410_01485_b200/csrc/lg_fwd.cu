@@ -46,13 +46,17 @@ lg_status launch_fwd(const Resolved& r, const WsLayout& w, const void* q, const 
                      float* lse, uint8_t* ws, cudaStream_t stream) {
   if (r.n_qtiles > 65535) return LG_ERR_UNSUPPORTED;
   const bool pairs = fwd_two_ctas(r);
-  if (r.late_reference && r.block == 64 && r.fsplit.len == 0) {
-    if (r.D == 128) return launch_fwd_t<128, 64, 2, false, true>(r, w, q, k, v, o, lse, ws, stream);
+  // (where a part of a device cannot hold a cluster the launch is refused, and the tiles stay whole)
+  if (r.late_reference && r.block == 64) {
+    if (r.D == 128) {
+      if (r.fsplit.len > 0 && launch_fwd_t<128, 64, 2, true, true>(r, w, q, k, v, o, lse, ws, stream) == LG_OK) return LG_OK;
+      return launch_fwd_t<128, 64, 2, false, true>(r, w, q, k, v, o, lse, ws, stream);
+    }
+    if (r.fsplit.len > 0 && launch_fwd_t<64, 64, 2, true, true>(r, w, q, k, v, o, lse, ws, stream) == LG_OK) return LG_OK;
     return pairs ? launch_fwd_t<64, 64, 1, false, true>(r, w, q, k, v, o, lse, ws, stream) : launch_fwd_t<64, 64, 2, false, true>(r, w, q, k, v, o, lse, ws, stream);
   }
 #define LG_FWD_CASE(DD, BB, NN) \
   if (r.D == DD && r.block == BB && pairs == (NN == 1)) return launch_fwd_t<DD, BB, NN, false>(r, w, q, k, v, o, lse, ws, stream);
-  // (where a part of a device cannot hold a cluster the launch is refused, and the tiles stay whole)
 #define LG_FWD_CUT_CASE(DD, BB) \
   if (r.fsplit.len > 0 && r.D == DD && r.block == BB && launch_fwd_t<DD, BB, 2, true>(r, w, q, k, v, o, lse, ws, stream) == LG_OK) return LG_OK;
   LG_FWD_CUT_CASE(128, 128)

@@ -513,7 +513,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
             }
             exp_half((m_ref == -INFINITY) ? 0.f : -m_ref);
           }
-         if constexpr (kRefine) {
+          if constexpr (kRefine) {
             // A reference that stays behind the maximum costs nothing in fp32, but the largest probability of a row is then a rounded number
             // like the others, and where one key has most of the weight its rounding is the row's error.  It cancels when the row is
             // divided by the rounded probabilities' sum.  (Chunk of 1500 tokens, 64 / 8 heads, uneven keys: O is 1.50e-3 off in the norm, of which
@@ -548,7 +548,8 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
     if (ok && p0 + p1 > 0 && qi - lane < a.L && qi - lane + 32 > a.q_start) {
       const bool mine = qi < a.L && qi >= a.q_start;
       tc_fence_after();
-      const float inv_l = l_run > 0.f ? 1.f / (kRefine ? l_run + c_run : l_run) : 0.f;
+      const bool some = kRefine ? l_run != 0.f : l_run > 0.f;      // (kRefine: a sum that is NaN stays NaN)
+      const float inv_l = some ? 1.f / (kRefine ? l_run + c_run : l_run) : 0.f;
       // rows leave through the slot's own Q tile (its last S product is done: it precedes the last P V in
       // the issuer's queue), 4 KB per warp, so that the stores cover whole rows (store_acc_64cols)
       uint8_t* stage = sQ + s * kTile + (warp & 3) * 4096;
@@ -562,7 +563,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
         });
       if (mine)
         a.lse[(static_cast<int64_t>(b) * a.Hq + h) * a.Lq + qi - a.q_start] =
-            l_run > 0.f ? (m_ref + log2f(l_run)) * 0.6931471805599453f : -INFINITY;
+            some ? (m_ref + log2f(l_run)) * 0.6931471805599453f : -INFINITY;
     }
   }
   tc_fence_before();
@@ -581,6 +582,11 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
             uint32_t reg[32];
             tmem_ld32(my_o + c, reg);
             tmem_ld_wait();
+            if constexpr (kRefine) {                       // a piece's own quotient, weighed by its unrounded sum like the others'
+              const float fit = l_run != 0.f ? l_run / (l_run + c_run) : 1.f;
+#pragma unroll
+              for (int x = 0; x < 32; ++x) reg[x] = __float_as_uint(__uint_as_float(reg[x]) * fit);
+            }
 #pragma unroll
             for (int x = 0; x < 32; x += 4)
               *reinterpret_cast<uint4*>(smem + row * FwdJoin<D>::kRow + (c + x) * 4) = make_uint4(reg[x], reg[x + 1], reg[x + 2], reg[x + 3]);

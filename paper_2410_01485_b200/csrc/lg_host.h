@@ -108,7 +108,7 @@ struct Resolved {          // validated, defaulted copy of lg_attn_params
   int kv_total;              // kv heads (times batch) of the whole problem: B * Hkv, more when the call works a group of its heads
   KvSplit split;             // how the dK/dV pass cuts its kv tiles (calls with a backward; see kv_split)
   FwdSplit fsplit;           // which super-tiles the forward cuts (see fwd_split)
-  bool late_reference;       // forward: the maxima of the rows are expected to rise often (see kFwdLateProb); whole tiles of 64-token blocks only
+  bool late_reference;       // forward: the maxima of the rows are expected to rise often (see kFwdLateProb); 64-token blocks only
 };
 
 // want_bwd: the call runs, prepares or sizes a backward; kv_total: kv heads of the whole problem when `p` is a group of
