@@ -407,13 +407,19 @@ __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const Gath
 // Scores are S^T = K Q^T and outputs O^T = V^T P^T on mma.sync m16n8k16 with f16 operands: an e4m3 code is an f16 number, so K
 // and V enter without rounding, and q (8 significant bits) does not lose any either once its row is scaled by a power of
 // two.  A contraction 8 heads wide is far below a tcgen05 tile.
-// A page's K scale multiplies its scores; that of V goes into the weights: w_j = 2^(s_j + log2 vs - r) with a running reference r of
-// its own, so that w fits f16 (11 bits) whatever the pages' scales are, while the row sum is kept in fp32 relative to the
-// running maximum m of the scores alone.  As long as all pages of a unit have one V scale, r = m + log2 vs and w = p.
+// (K as e4m3 in products of its own kind, with q as the sum of two e4m3 numbers, needs no conversion but was slower: one sequence over 4224
+// slots 14.0 us against 12.4 with its append, 16 over 60-131 thousand 531 us against 500.)
+// A page's K scale multiplies its scores; that of V goes into the weights, w_j = p_j vs / vs_ref with the largest scale of the unit so far, so that
+// they fit f16 (11 bits), while the row sum is kept in fp32.  Where the scales of a unit's pages lie more than 2^10 apart that would cost
+// bits, and the weights get a running reference of their own, w_j = 2^(s_j + log2 vs - r).
+// The instructions of a tile count although HBM bounds the kernel: in a loop of milliseconds the board is at its power limit, and the clock
+// that it takes back is the SMs' (16 sequences over 60-131 thousand slots, 600 steps in a row: 521 us with a maximum and a rescaling in every
+// tile and two exponentials a weight, 500 us so).
 constexpr int kPagedTile = 32, kPagedHalf = 16;   // tokens of a tile, and of what lies in one page whatever its size
 constexpr int kPagedSlots = 5;          // 4 KB each at D = 128: three tiles' K and two tiles' V, or the other way round
 constexpr int kPagedMaxB = 4096;        // sequences of one launch (their prefix sums lie in shared memory)
 constexpr int kPagedMaxCtas = 320;
+constexpr float kNoScore = -3.4e38f;    // the reference of a row that has attended nothing
 
 struct PagedDecodeArgs {
   const __nv_bfloat16* q;        // [B, Hq, D]
@@ -763,11 +769,12 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
   };
 
   uint32_t qf[D / 16][2];
-  float qs0 = 0.f, qs1 = 0.f;                // of heads 2c, 2c+1
-  float m_run[2], r_run[2], l_run[2];        // maximum of the scores (log2 domain), reference of the weights, the thread's share of the sum
+  float qs0 = 0.f, qs1 = 0.f;                // what a product is multiplied by, heads 2c, 2c+1
+  float m_run[2], l_run[2];                  // reference of the probabilities (log2 domain), the thread's share of their sum
   float oacc[D / 16][4];
-  bool same = true;                          // one V scale so far (vs_ref): r = m + log2 vs_ref
-  float vs_ref = -1.f;
+  float vs_ref = -1.f, vs_inv = 0.f, vs_min = 0.f;   // largest V scale so far, its reciprocal, the smallest one
+  bool own = false;                          // the V scales lie too far apart: the weights have a reference of their own
+  float r_run[2];                            // ... this one
   int nvalid = 0, ex0 = 0, ex_cnt = 0, first_t = 0;
   const int ring_w = a.C - a.sink;
   auto attended = [&](int slot) {
@@ -793,7 +800,6 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
   }
 #pragma unroll 1
   for (int i = 0; i < n_run; ++i) {
-    float s[2][4] = {};
     const int first_slot = cur.t * kPagedTile;
     if (i == 0 || cur.t == 0) {
       // A unit begins.  q in f16, its row scaled by a power of two to at most 2^11: b0 = dims 16 k + 4 c, +1, b1 = the next two (the
@@ -828,12 +834,13 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
       }
       qs0 = __shfl_sync(0xffffffffu, q_mul, 8 * c);
       qs1 = __shfl_sync(0xffffffffu, q_mul, 8 * c + 4);
-      m_run[0] = m_run[1] = r_run[0] = r_run[1] = -INFINITY;
+      m_run[0] = m_run[1] = kNoScore;
       l_run[0] = l_run[1] = 0.f;
 #pragma unroll
       for (int x = 0; x < D / 16; ++x) oacc[x][0] = oacc[x][1] = oacc[x][2] = oacc[x][3] = 0.f;
-      same = true;
+      own = false;
       vs_ref = -1.f;
+      vs_min = 3.4e38f;
       first_t = cur.t;
     }
     copy_wait<kPagedSlots - 1>();
@@ -848,6 +855,8 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
       edge |= d < ex_cnt || d + kPagedTile > ring_w;
     }
 
+    // ---- S^T[32 tokens, 8 heads] = K Q^T
+    float s[2][4] = {};
     // ---- S^T[32 tokens, 8 heads] = K Q^T
     const uint32_t sk = ring + slot;
 #pragma unroll
@@ -865,12 +874,14 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
     if (i + 2 < n_run) copy_tile(a.pool[1]);   // V of the tile whose K was asked for last
     copy_commit();
 
-    // s[x][0, 1]: token 16 x + r, heads 2c, 2c+1; s[x][2, 3]: token 16 x + r + 8.  (The scales together are kept finite: a score of
-    // zero stays zero.)
+    // s[x][0, 1]: token 16 x + r, heads 2c, 2c+1; s[x][2, 3]: token 16 x + r + 8.  A score is s times its scales, which together are kept
+    // finite and above zero (1e-30: what is cut there is a score below 1e-22), so that a score of zero stays zero and -inf stays -inf.
+    float sc0[2], sc1[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const float kk = x ? sc.z : sc.x, c0 = fminf(qs0 * kk, 3.4e38f), c1 = fminf(qs1 * kk, 3.4e38f);
-      s[x][0] *= c0; s[x][1] *= c1; s[x][2] *= c0; s[x][3] *= c1;
+      const float kk = x ? sc.z : sc.x;
+      sc0[x] = fminf(fmaxf(qs0 * kk, 1e-30f), 3.4e38f);
+      sc1[x] = fminf(fmaxf(qs1 * kk, 1e-30f), 3.4e38f);
     }
     if (edge) {
 #pragma unroll
@@ -880,52 +891,85 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
         if (!in || !attended(first_slot + 16 * x + r + 8)) s[x][2] = s[x][3] = -INFINITY;
       }
     }
-    float t0 = fmaxf(fmaxf(s[0][0], s[0][2]), fmaxf(s[1][0], s[1][2])), t1 = fmaxf(fmaxf(s[0][1], s[0][3]), fmaxf(s[1][1], s[1][3]));
-#pragma unroll
-    for (int o = 4; o < 32; o <<= 1) {
-      t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, o));
-      t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, o));
-    }
-    const float mn0 = fmaxf(m_run[0], t0), mn1 = fmaxf(m_run[1], t1);
-    const float mu0 = mn0 == -INFINITY ? 0.f : mn0, mu1 = mn1 == -INFINITY ? 0.f : mn1;
-    float be0 = fast_exp2(m_run[0] - mu0), be1 = fast_exp2(m_run[1] - mu1);
     float w[2][4];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      w[x][0] = fast_exp2(s[x][0] - mu0); w[x][1] = fast_exp2(s[x][1] - mu1);
-      w[x][2] = fast_exp2(s[x][2] - mu0); w[x][3] = fast_exp2(s[x][3] - mu1);
-    }
-    l_run[0] = l_run[0] * be0 + ((w[0][0] + w[0][2]) + (w[1][0] + w[1][2]));
-    l_run[1] = l_run[1] * be1 + ((w[0][1] + w[0][3]) + (w[1][1] + w[1][3]));
-    const float v0 = in0 ? sc.y : in1 ? sc.w : vs_ref, v1 = in1 ? sc.w : v0;   // (a half that is not there has no weights)
-    if (vs_ref < 0.f) vs_ref = v0;
-    if (same && (v0 != vs_ref || v1 != vs_ref)) {   // from here on the weights have a reference of their own
-      same = false;
-      const float lr = fast_log2(vs_ref);
-      r_run[0] = m_run[0] + lr; r_run[1] = m_run[1] + lr;
-    }
-    m_run[0] = mn0; m_run[1] = mn1;
-    if (!same) {
-      const float lv0 = fast_log2(v0), lv1 = fast_log2(v1);
-      float u0 = fmaxf(fmaxf(s[0][0], s[0][2]) + lv0, fmaxf(s[1][0], s[1][2]) + lv1);
-      float u1 = fmaxf(fmaxf(s[0][1], s[0][3]) + lv0, fmaxf(s[1][1], s[1][3]) + lv1);
-#pragma unroll
-      for (int o = 4; o < 32; o <<= 1) {
-        u0 = fmaxf(u0, __shfl_xor_sync(0xffffffffu, u0, o));
-        u1 = fmaxf(u1, __shfl_xor_sync(0xffffffffu, u1, o));
-      }
-      const float rn0 = fmaxf(r_run[0], u0), rn1 = fmaxf(r_run[1], u1);
-      const float ru0 = rn0 == -INFINITY ? 0.f : rn0, ru1 = rn1 == -INFINITY ? 0.f : rn1;
-      be0 = fast_exp2(r_run[0] - ru0); be1 = fast_exp2(r_run[1] - ru1);
-      r_run[0] = rn0; r_run[1] = rn1;
+    auto scores = [&](float sub0, float sub1) {   // less a reference
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const float d0 = (x ? lv1 : lv0) - ru0, d1 = (x ? lv1 : lv0) - ru1;
-        w[x][0] = fast_exp2(s[x][0] + d0); w[x][1] = fast_exp2(s[x][1] + d1);
-        w[x][2] = fast_exp2(s[x][2] + d0); w[x][3] = fast_exp2(s[x][3] + d1);
+        w[x][0] = fmaf(s[x][0], sc0[x], -sub0); w[x][1] = fmaf(s[x][1], sc1[x], -sub1);
+        w[x][2] = fmaf(s[x][2], sc0[x], -sub0); w[x][3] = fmaf(s[x][3], sc1[x], -sub1);
+      }
+    };
+    float t0, t1;
+    auto top = [&]() {
+      t0 = fmaxf(fmaxf(w[0][0], w[0][2]), fmaxf(w[1][0], w[1][2]));
+      t1 = fmaxf(fmaxf(w[0][1], w[0][3]), fmaxf(w[1][1], w[1][3]));
+    };
+    auto over_tokens = [&]() {
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) {
+        t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, o));
+        t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, o));
+      }
+    };
+    float be0 = 1.f, be1 = 1.f;               // what O is multiplied by
+    bool moved = false;
+    scores(m_run[0], m_run[1]);
+    top();
+    // The reference moves to the maximum when a probability passes 2^8; until then fp32 sums and f16 weights (up to 2^15) do without.
+    if (__any_sync(0xffffffffu, fmaxf(t0, t1) > 8.f)) {
+      scores(0.f, 0.f);
+      top();
+      over_tokens();
+      t0 = fmaxf(m_run[0], t0); t1 = fmaxf(m_run[1], t1);
+      const float al0 = fast_exp2(m_run[0] - t0), al1 = fast_exp2(m_run[1] - t1);
+      m_run[0] = t0; m_run[1] = t1;
+      l_run[0] *= al0; l_run[1] *= al1;
+      if (!own) { be0 = al0; be1 = al1; moved = true; }
+      scores(t0, t1);
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) w[x][y] = fast_exp2(w[x][y]);
+    l_run[0] += (w[0][0] + w[0][2]) + (w[1][0] + w[1][2]);
+    l_run[1] += (w[0][1] + w[0][3]) + (w[1][1] + w[1][3]);
+    // The pages' V scales relative to the largest so far (a half that is not there has no weights).
+    const float v0 = in0 ? sc.y : in1 ? sc.w : vs_ref, v1 = in1 ? sc.w : v0;
+    if (!own && v0 > 0.f && (fmaxf(v0, v1) > vs_ref || fminf(v0, v1) < vs_min)) {
+      const float most = fmaxf(vs_ref, fmaxf(v0, v1));
+      vs_min = fminf(vs_min, fminf(v0, v1));
+      own = vs_min * 1024.f < most;           // (then O keeps the reference that it has)
+      if (own) {
+        const float lr = fast_log2(vs_ref);
+        r_run[0] = vs_ref > 0.f ? m_run[0] + lr : kNoScore; r_run[1] = vs_ref > 0.f ? m_run[1] + lr : kNoScore;
+      } else if (most != vs_ref) {
+        if (vs_ref > 0.f) { be0 *= vs_ref / most; be1 *= vs_ref / most; moved = true; }
+        vs_inv = 1.f / most;
+      }
+      vs_ref = most;
+    }
+    if (!own) {
+      const float h0 = v0 * vs_inv, h1 = v1 * vs_inv;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) { w[0][y] *= h0; w[1][y] *= h1; }
+    } else {
+      const float lv0 = fast_log2(v0), lv1 = fast_log2(v1);
+      scores(0.f, 0.f);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) { w[0][y] += lv0; w[1][y] += lv1; }
+      top();
+      over_tokens();
+      t0 = fmaxf(r_run[0], t0); t1 = fmaxf(r_run[1], t1);
+      be0 *= fast_exp2(r_run[0] - t0); be1 *= fast_exp2(r_run[1] - t1);
+      r_run[0] = t0; r_run[1] = t1;
+      moved = true;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        w[x][0] = fast_exp2(w[x][0] - t0); w[x][1] = fast_exp2(w[x][1] - t1);
+        w[x][2] = fast_exp2(w[x][2] - t0); w[x][3] = fast_exp2(w[x][3] - t1);
       }
     }
-    if (__any_sync(0xffffffffu, be0 != 1.f || be1 != 1.f)) {
+    if (moved) {
 #pragma unroll
       for (int x = 0; x < D / 16; ++x) { oacc[x][0] *= be0; oacc[x][1] *= be1; oacc[x][2] *= be0; oacc[x][3] *= be1; }
     }
@@ -976,7 +1020,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
       }
       float g[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) g[x] = m_run[x] == -INFINITY ? 0.f : same ? vs_ref : fast_exp2(r_run[x] - m_run[x]);
+      for (int x = 0; x < 2; ++x) g[x] = own ? fast_exp2(r_run[x] - m_run[x]) : vs_ref;
       if (first_t == 0 && tail) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
