@@ -58,7 +58,9 @@ lg_status resolve(const lg_attn_params* p, Resolved* r, bool want_bwd, int kv_to
   r->pat.nB = (p->L + p->block - 1) / p->block;
   r->pat.mode = p->mode;
   r->pat.ns = r->pat.nw = r->pat.stride = r->pat.nl = 0;
-  r->late_reference = false;
+  r->views = nullptr;
+  r->ent_stride = 0;
+  r->shared_lists = true;
   r->pat.doc_start = nullptr;
   r->pat.block = p->block;
   r->exact_w = 0;
@@ -391,34 +393,55 @@ static lg_status plan_chunk(const lg_decode_params* p, int32_t T, int64_t n_befo
 }
 
 // ---- a chunk served against the paged cache ---------------------------------------------------
-// One launch ahead of the attention kernel: block 0 builds the forward's schedule (a warp per super-tile, then their ranks, as
-// sched_build_kernel and sched_order_kernel do) and checks the tables, the other blocks copy (paged_linearise).  Block 0 alone writes the header, so that
-// what it finds missing is not wiped.
-constexpr int kChunkMaxTiles = 64;   // super-tiles that one block ranks; longer chunks have their schedule built by the two launches
-__global__ void __launch_bounds__(kGatherThreads) chunk_prepare_kernel(const SchedArgs a, const PagedLinearise l, int blocks_x, int build) {
+// One launch ahead of the attention kernel: block 0 checks the tables and writes the views, a block per sequence builds its schedule (a warp per
+// super-tile, then their ranks, as sched_build_kernel and sched_order_kernel do, without the blocks that lie in its gap), the others copy
+// (paged_linearise).  Block 0 alone writes the header, so that what it finds missing is not wiped.
+constexpr int kChunkMaxTiles = 64;   // super-tiles that one block ranks; longer chunks have their schedule, one for all, built by the two launches
+__global__ void __launch_bounds__(kGatherThreads) chunk_prepare_kernel(const SchedArgs a, const PagedLinearise l, ChunkView* views, int64_t ent_stride,
+                                                                       int blocks_x, int lists, int begin) {
   pdl_trigger();
   pdl_wait();
-  if (blockIdx.x > 0) {
-    const int64_t w = blockIdx.x - 1, bh = w / blocks_x;
+  if (static_cast<int>(blockIdx.x) > lists) {
+    const int64_t w = blockIdx.x - 1 - lists, bh = w / blocks_x;
     const int b = static_cast<int>(bh / l.Hkv);
     paged_linearise(l, (w - bh * blocks_x) * kGatherThreads + threadIdx.x, static_cast<int>(bh - static_cast<int64_t>(b) * l.Hkv), b);
     return;
   }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (build) {
-    if (threadIdx.x == 0) header_begin(a.header);
-    for (int t = warp; t < a.n_stiles; t += kGatherThreads / 32) {
-      const int r0 = a.st_row0 + 2 * a.R * t, off = row_start(a.p, r0) - row_start(a.p, a.st_row0);
-      const int n = merge_rows(a.p, r0, 2 * a.R, 16, a.sq_ent + off);
-      if (lane == 0) { a.sq_off[t] = off; a.sq_cnt[t] = n; }
-    }
+  if (blockIdx.x == 0) {
+    if (begin && threadIdx.x == 0) header_begin(a.header);
+    for (int b = threadIdx.x; b < l.B; b += kGatherThreads) views[b] = chunk_view(l.kept, l.sink, l.seq[b]);
+    const bool missing = paged_entry_missing(l, kGatherThreads);
+    if (missing && threadIdx.x == 0) atomicCAS(l.error_word, 0u, kPageError);
+    return;
   }
-  const bool missing = paged_entry_missing(l, kGatherThreads);   // (its barrier also stands between the counts and the ranks)
-  if (missing && threadIdx.x == 0) atomicCAS(l.error_word, 0u, kPageError);
-  if (!build) return;
+  __shared__ int32_t cnt[kChunkMaxTiles];
+  const int b = blockIdx.x - 1;
+  const ChunkView view = chunk_view(l.kept, l.sink, l.seq[b]);
+  int32_t* ent = a.sq_ent + b * ent_stride;
+  const int origin = row_start(a.p, a.st_row0);
   for (int t = warp; t < a.n_stiles; t += kGatherThreads / 32) {
-    const int rank = rank_of(a.sq_cnt, a.n_stiles, t);
-    if (lane == 0) a.sq_order[rank] = TileRec{a.sq_off[t], a.sq_cnt[t], t, -1};
+    const int r0 = a.st_row0 + 2 * a.R * t;
+    int32_t* mine = ent + (row_start(a.p, r0) - origin);
+    int n = merge_rows(a.p, r0, 2 * a.R, 16, mine);
+    if (view.first > 0) {
+      int left = 0;                                              // entries move to the front, 32 at a time
+      __syncwarp();
+      for (int i = 0; i < n; i += 32) {
+        const int e = i + lane < n ? mine[i + lane] : -1;
+        const unsigned m = __ballot_sync(0xffffffffu, e >= 0 && chunk_block_held(view, l.sink, e >> 4));
+        if ((m >> lane) & 1) mine[left + __popc(m & ((1u << lane) - 1))] = e;
+        left += __popc(m);
+        __syncwarp();
+      }
+      n = left;
+    }
+    if (lane == 0) cnt[t] = n;
+  }
+  __syncthreads();
+  for (int t = warp; t < a.n_stiles; t += kGatherThreads / 32) {
+    const int rank = rank_of(cnt, a.n_stiles, t);
+    if (lane == 0) a.sq_order[static_cast<int64_t>(b) * a.n_stiles + rank] = TileRec{row_start(a.p, a.st_row0 + 2 * a.R * t) - origin, cnt[t], t, -1};
   }
 }
 
@@ -665,8 +688,12 @@ lg_status lg_chunk_prefill(const lg_decode_params* p, const void* q_chunk, const
   return launch_fwd(c.r, c.w, q_chunk, k_lin, v_lin, o, lse, ws, st);
 }
 
-// The sequences are taken in runs of neighbours that keep as many tokens (and, with a block-aligned window, have the same phase): the
-// attention kernel's rows are counted from the number of kept tokens.  Rings that are full, and a batch at one position, are one run.
+// The sequences are taken in runs of neighbours, a run a launch of the attention kernel, whose rows are counted from the number of kept tokens.
+// Sequences that hold fewer than the run's fullest have a gap (lg_paged.h), so that any positions make one run, but for two cases: a chunk of so
+// many super-tiles that its schedule is one for all, and a sequence whose sink is not yet full while the chunk is longer than its window (a
+// token of the chunk that belongs to the sink would leave it).  There a run is what holds equally many.  Against a run for
+// every position: 3 sequences of 203 tokens, 16 heads of 64, window 1024: 53.7 -> 25.5 us, 16 of them 278 -> 62; 16 of 512 tokens, 32 heads of 128, window
+// 4096: 811 -> 423; a full ring and four that hold 100 to 300 tokens, 1500 new ones each: 270 -> 232.
 namespace {
 lg_decode_params ring_of(const lg_paged_params* p, int B) {
   lg_decode_params d;
@@ -674,29 +701,54 @@ lg_decode_params ring_of(const lg_paged_params* p, int B) {
   d.sink_tokens = p->sink_tokens; d.window_tokens = p->window_tokens; d.block_tokens = p->block_tokens; d.scale = p->scale;
   return d;
 }
-int chunk_run(const lg_paged_params* p, const int64_t* n, int b) {   // end of the run that starts at sequence b
+struct ChunkRun { int end; int64_t kept; };
+ChunkRun chunk_run(const lg_paged_params* p, int32_t T, const int64_t* n, int b) {   // the run that starts at sequence b
   const int64_t cap = static_cast<int64_t>(p->sink_tokens) + p->window_tokens;
-  auto same = [&](int64_t x, int64_t y) {
-    if ((x < cap ? x : cap) != (y < cap ? y : cap)) return false;
-    return p->block_tokens <= 0 || x < cap || (x - cap) % p->block_tokens == (y - cap) % p->block_tokens;
-  };
-  int e = b + 1;
-  while (e < p->B && same(n[b], n[e])) ++e;
-  return e;
+  auto held = [&](int x) { return n[x] < cap ? n[x] : cap; };
+  const bool own_lists = T <= 256 * kChunkMaxTiles - 63, all_near = T <= p->window_tokens - (p->block_tokens > 0 ? p->block_tokens - 1 : 0);
+  auto free = [&](int x) { return own_lists && (all_near || held(x) >= p->sink_tokens); };
+  ChunkRun r{b + 1, held(b)};
+  bool equal = true;
+  for (; r.end < p->B; ++r.end) {
+    if (equal && held(r.end) == r.kept) continue;
+    if (!free(r.end) || !free(b)) break;
+    equal = false;
+    if (held(r.end) > r.kept) r.kept = held(r.end);
+    if (r.kept < p->sink_tokens) r.kept = p->sink_tokens;     // (a gap starts behind the sink at the earliest)
+  }
+  return r;
+}
+// The plan of a run: that of a ring at the position of its fullest sequence, then the views and the sequences' own lists.
+lg_status plan_run(const lg_paged_params* p, int32_t T, const ChunkRun& run, int b, ChunkPlan* c, size_t* views) {
+  const lg_decode_params d = ring_of(p, run.end - b);
+  const lg_status s = plan_chunk(&d, T, run.kept, c);
+  if (s != LG_OK) return s;
+  *views = align_up(c->total, 256);
+  c->total = *views + align_up(static_cast<size_t>(d.B) * sizeof(ChunkView), 256);
+  c->r.shared_lists = c->r.n_stiles > kChunkMaxTiles;
+  if (!c->r.shared_lists) {
+    c->r.ent_stride = row_start(c->r.pat, c->r.pat.nB) - row_start(c->r.pat, c->r.st_row0);
+    c->w.sq_order = c->total;
+    c->w.sq_ent = c->w.sq_order + align_up(static_cast<size_t>(d.B) * c->r.n_stiles * sizeof(TileRec), 256);
+    c->total = c->w.sq_ent + align_up(static_cast<size_t>(d.B) * c->r.ent_stride * sizeof(int32_t), 256);
+  }
+  return LG_OK;
 }
 lg_status paged_chunk_bytes(const lg_paged_params* p, int32_t T, const int64_t* n, size_t* total) {
   const lg_status s = check_paged(p);
   if (s != LG_OK) return s;
   if (!n) return LG_ERR_INVALID_ARG;
+  for (int b = 0; b < p->B; ++b)
+    if (n[b] < 0) return LG_ERR_INVALID_ARG;
   *total = 0;
   for (int b = 0; b < p->B;) {
-    const int e = chunk_run(p, n, b);
-    const lg_decode_params d = ring_of(p, e - b);
+    const ChunkRun run = chunk_run(p, T, n, b);
     ChunkPlan c;
-    const lg_status r = plan_chunk(&d, T, n[b], &c);
+    size_t views;
+    const lg_status r = plan_run(p, T, run, b, &c, &views);
     if (r != LG_OK) return r;
     if (c.total > *total) *total = c.total;
-    b = e;
+    b = run.end;
   }
   return LG_OK;
 }
@@ -726,49 +778,53 @@ lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, 
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const int stride = paged_table_stride(p);
   for (int b = 0; b < p->B;) {
-    const int e = chunk_run(p, n_tokens_before, b);
-    const int64_t n = n_tokens_before[b], q_at = static_cast<int64_t>(b) * p->Hq * T;
-    const lg_decode_params d = ring_of(p, e - b);
+    const ChunkRun run = chunk_run(p, T, n_tokens_before, b);
+    const int e = run.end;
+    const int64_t q_at = static_cast<int64_t>(b) * p->Hq * T;
     ChunkPlan c;
-    if ((s = plan_chunk(&d, T, n, &c)) != LG_OK) return s;
-    c.r.late_reference = true;
-    const bool one = c.r.n_stiles <= kChunkMaxTiles;
-    if (!one && (s = prepare_workspace(c.r, c.w, ws, 1, true, 0, st)) != LG_OK) return s;
+    size_t o_views;
+    if ((s = plan_run(p, T, run, b, &c, &o_views)) != LG_OK) return s;
+    ChunkView* views = reinterpret_cast<ChunkView*>(ws + o_views);
+    c.r.views = views;
+    const bool own = !c.r.shared_lists;
+    if (!own && (s = prepare_workspace(c.r, c.w, ws, 1, true, 0, st)) != LG_OK) return s;
     SchedArgs sched{};
     sched.p = c.r.pat;
     sched.header = reinterpret_cast<WsHeader*>(ws);
     sched.R = 128 / c.r.block;
     sched.n_stiles = c.r.n_stiles; sched.st_row0 = c.r.st_row0;
-    sched.sq_off = reinterpret_cast<int32_t*>(ws + c.w.sq_off); sched.sq_cnt = reinterpret_cast<int32_t*>(ws + c.w.sq_cnt);
-    sched.sq_ent = reinterpret_cast<int32_t*>(ws + c.w.sq_ent); sched.sq_order = reinterpret_cast<TileRec*>(ws + c.w.sq_order);
     PagedLinearise l;
     l.pool[0] = k_pool; l.pool[1] = v_pool; l.scale[0] = k_scale; l.scale[1] = v_scale;
     l.error_word = reinterpret_cast<unsigned int*>(ws);
     l.Hkv = p->Hkv; l.D = p->D; l.T = T; l.kept = c.kept; l.sink = p->sink_tokens; l.window = p->window_tokens;
-    // the chunk's first token sees the furthest back: behind the sink the rows v with (kept + phase) / block - (v + phase) / block < window / block
-    l.hidden = 0;
-    if (p->block_tokens > 0) {
-      const int first = ((c.kept + c.r.win_phase) / p->block_tokens - p->window_tokens / p->block_tokens + 1) * p->block_tokens - c.r.win_phase;
-      l.hidden = first < 0 ? 0 : first;
-    } else if (c.kept == p->sink_tokens + p->window_tokens) {
-      l.hidden = p->sink_tokens + 1;   // (a full ring: its oldest token has left the window)
-    }
     l.page_shift = page_shift(p->page_tokens); l.num_pages = p->num_pages; l.stride = stride;
     __nv_bfloat16* lin[2] = {reinterpret_cast<__nv_bfloat16*>(ws + c.o_k), reinterpret_cast<__nv_bfloat16*>(ws + c.o_v)};
     for (int x = b; x < e; x += kLineariseSeqs) {
       l.B = e - x < kLineariseSeqs ? e - x : kLineariseSeqs;
-      for (int y = 0; y < l.B; ++y)
-        l.ring0[y] = c.kept > p->sink_tokens ? static_cast<int>((n_tokens_before[x + y] - c.kept) % p->window_tokens) : 0;
+      const int64_t cap = static_cast<int64_t>(p->sink_tokens) + p->window_tokens;
+      const int bt = p->block_tokens;
+      for (int y = 0; y < l.B; ++y) {
+        const int64_t n = n_tokens_before[x + y];
+        ChunkSeq& sq = l.seq[y];
+        sq.held = static_cast<int>(n < cap ? n : cap);
+        sq.ring0 = static_cast<int>((n - sq.held) % p->window_tokens);
+        sq.phase = bt > 0 ? static_cast<int>(((n - c.kept) % bt + bt) % bt) : 0;
+        // the chunk's first token sees the furthest back: rows v with (kept + phase) / block - (v + phase) / block < window / block, or the last `window`
+        sq.seen = bt > 0 ? ((c.kept + sq.phase) / bt - p->window_tokens / bt + 1) * bt - sq.phase : c.kept - p->window_tokens + 1;
+      }
       for (int y = 0; y < 2; ++y) {
         l.chunk[y] = static_cast<const __nv_bfloat16*>(y ? v_chunk : k_chunk) + static_cast<int64_t>(x) * p->Hkv * T * p->D;
         l.lin[y] = lin[y] + static_cast<int64_t>(x - b) * p->Hkv * c.ap.L * p->D;
       }
       l.table = block_table + static_cast<int64_t>(x) * stride;
+      sched.sq_order = reinterpret_cast<TileRec*>(ws + c.w.sq_order) + static_cast<int64_t>(x - b) * c.r.n_stiles;
+      sched.sq_ent = reinterpret_cast<int32_t*>(ws + c.w.sq_ent) + (x - b) * c.r.ent_stride;
       const int64_t blocks_x = (static_cast<int64_t>(c.ap.L) * (p->D / 16) + kGatherThreads - 1) / kGatherThreads;
-      const int64_t blocks = blocks_x * p->Hkv * l.B + 1;
+      const int lists = own ? l.B : 0;
+      const int64_t blocks = blocks_x * p->Hkv * l.B + 1 + lists;
       if (blocks > 0x7fffffff) return LG_ERR_UNSUPPORTED;
-      if (launch_kernel(true, chunk_prepare_kernel, dim3(static_cast<unsigned>(blocks)), kGatherThreads, 0, st, sched, l, static_cast<int>(blocks_x),
-                        one && x == b ? 1 : 0) != cudaSuccess)
+      if (launch_kernel(true, chunk_prepare_kernel, dim3(static_cast<unsigned>(blocks)), kGatherThreads, 0, st, sched, l, views + (x - b),
+                        c.r.ent_stride, static_cast<int>(blocks_x), lists, own && x == b ? 1 : 0) != cudaSuccess)
         return LG_ERR_CUDA;
     }
     if ((s = launch_fwd(c.r, c.w, static_cast<const __nv_bfloat16*>(q_chunk) + q_at * p->D, lin[0], lin[1],

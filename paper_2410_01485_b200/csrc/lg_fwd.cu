@@ -4,7 +4,7 @@
 
 namespace lg {
 
-template <int D, int BS, int NB, bool kSplit, bool kRefine = false>
+template <int D, int BS, int NB, bool kSplit, bool kPaged = false>
 static lg_status launch_fwd_t(const Resolved& r, const WsLayout& w, const void* q, const void* k, const void* v,
                               void* o, float* lse, uint8_t* ws, cudaStream_t stream) {
   CUtensorMap tq, tk, tv;
@@ -29,10 +29,13 @@ static lg_status launch_fwd_t(const Resolved& r, const WsLayout& w, const void* 
   a.win_block = r.win_block; a.win_phase = r.win_phase;
   a.doc_start = r.doc_start;
   a.scale_log2 = r.scale * 1.4426950408889634f;
-  a.max_prob = kRefine ? kFwdLateProb : kFwdMaxProb;
+  a.max_prob = kPaged ? kFwdLateProb : kFwdMaxProb;
   a.head_group = head_group(r, r.B * r.Hq);
   a.split = r.fsplit;
-  auto kern = fwd_kernel<D, BS, NB, kSplit, kRefine>;
+  a.views = r.views;
+  a.ent_stride = r.shared_lists ? 0 : r.ent_stride;
+  a.order_stride = r.shared_lists ? 0 : r.n_stiles;
+  auto kern = fwd_kernel<D, BS, NB, kSplit, kPaged>;
   constexpr int smem = FwdSmem<D>::kTotal;
   static std::atomic<bool> allowed[kMaxDevices];
   // cut tiles: clusters of as many CTAs as a tile has places; the last cluster is filled up
@@ -47,7 +50,7 @@ lg_status launch_fwd(const Resolved& r, const WsLayout& w, const void* q, const 
   if (r.n_qtiles > 65535) return LG_ERR_UNSUPPORTED;
   const bool pairs = fwd_two_ctas(r);
   // (where a part of a device cannot hold a cluster the launch is refused, and the tiles stay whole)
-  if (r.late_reference && r.block == 64) {
+  if (r.views && r.block == 64) {
     if (r.D == 128) {
       if (r.fsplit.len > 0 && launch_fwd_t<128, 64, 2, true, true>(r, w, q, k, v, o, lse, ws, stream) == LG_OK) return LG_OK;
       return launch_fwd_t<128, 64, 2, false, true>(r, w, q, k, v, o, lse, ws, stream);

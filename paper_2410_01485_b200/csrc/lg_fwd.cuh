@@ -31,6 +31,7 @@
 #pragma once
 #include <cuda.h>
 #include "lg_common.cuh"
+#include "lg_paged.h"
 #include "lg_pattern.h"
 
 namespace lg {
@@ -64,6 +65,10 @@ struct FwdArgs {
   float max_prob;            // a half's probabilities may grow to this (relative to the row's reference) before the reference moves
   int head_group;            // heads whose CTAs run side by side (cta_coords); >= gridDim.x: all of them
   FwdSplit split;            // tiles cut along their keys
+  // chunks over the paged cache (kPaged): the sequences' views, and how far the lists of one lie behind those of the one before
+  const ChunkView* views;
+  int64_t ent_stride;
+  int order_stride;
 };
 
 constexpr int kFwdTmaWarp = 8, kFwdMmaWarp0 = 9;
@@ -149,8 +154,8 @@ __device__ __forceinline__ void fwd_join(const FwdArgs& a, uint32_t base, uint32
   else fwd_join_rows<D, 8, 2>(a, base, n_segs, b, h, row0, first, end, step, c);
 }
 
-// kRefine: O is divided by the sum of the probabilities as they were rounded to bf16 where they weigh, the LSE by that of the unrounded ones (below).
-template <int D, int BS, int NB /* score buffers per slot */, bool kSplit, bool kRefine = false>
+// kPaged: a chunk over the paged cache.  Its sequences have their own lists and views, and O is divided by the sum of the probabilities as they were rounded to bf16 where they weigh, the LSE by that of the unrounded ones (below).
+template <int D, int BS, int NB /* score buffers per slot */, bool kSplit, bool kPaged = false>
 __global__ void __launch_bounds__(kFwdThreads, fwd_ctas_per_sm(NB))
 fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
            const __grid_constant__ CUtensorMap tm_v, const FwdArgs a) {
@@ -196,7 +201,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
   } else {
     cta_coords(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x, gridDim.y, a.head_group, cta_x, cta_y);
   }
-  const TileRec rec = load_rec(a.order + cta_y);
+  const TileRec rec = load_rec(a.order + (kPaged ? static_cast<int64_t>(cta_x / a.Hq) * a.order_stride : 0) + cta_y);
   if (!lists_match(a.error_word, a.expect_fp, a.expect_fp2, 1u)) return;
   uint8_t* sQ = smem + SM::oQ;
   uint8_t* sK = smem + SM::oK;
@@ -206,7 +211,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
   const int b = cta_x / a.Hq, h = cta_x % a.Hq, hk = h / a.G;
   const int ent_off = checked(rec.off, 0, a.n_list, a.error_word, 101);
   int n_ent = checked(rec.cnt, 0, a.n_list - ent_off, a.error_word, 102);
-  const int32_t* ent = a.tile_ent + ent_off;
+  const int32_t* ent = a.tile_ent + ent_off + (kPaged ? b * a.ent_stride : 0);
   const int row0 = a.row_origin + tile * 256;
   int n_steps = (BS == 128) ? n_ent : (n_ent + 1) / 2;
   const int n_segs = kSplit && cut ? fwd_pieces(a.split, n_steps) : 1;
@@ -257,7 +262,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
   // of a softmax thread's row:
   float m_ref = -INFINITY;   // reference maximum (scaled, log2 domain) the probabilities are relative to
   float l_run = 0.f;
-  float c_run = 0.f;         // kRefine: the rounded probabilities' sum less l_run, over the halves where it was looked at
+  float c_run = 0.f;         // kPaged: the rounded probabilities' sum less l_run, over the halves where it was looked at
   int p0 = 0, p1 = 0;        // P tiles published per score buffer (barrier phases)
   if (warp == kFwdTmaWarp) {
     // ------------------------------ TMA producer ------------------------------------------
@@ -395,9 +400,12 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
     // document (0 without documents)
     const int dstart = (a.doc_start && qi < a.L && qi >= a.q_start) ? a.doc_start[static_cast<int64_t>(b) * a.L + qi] : 0;
     // oldest key position the window lets this row see (blocks outside the sink)
-    const int win_lo = a.win_block > 0
-                           ? ((qi + a.win_phase) / a.win_block - a.exact_w / a.win_block + 1) * a.win_block - a.win_phase
-                           : qi - a.exact_w + 1;
+    int phase = a.win_phase, first = 0, sink_end = 0;        // (kPaged: of my sequence)
+    if constexpr (kPaged) { const ChunkView view = a.views[b]; phase = view.phase; first = view.first; sink_end = view.sink_end; }
+    int win_lo = a.win_block > 0
+                     ? ((qi + phase) / a.win_block - a.exact_w / a.win_block + 1) * a.win_block - phase
+                     : qi - a.exact_w + 1;
+    if constexpr (kPaged) win_lo = max(win_lo, first);
     // every P V product issued so far has completed (at most one per buffer can still be running)
     auto wait_o = [&](uint32_t site) {
       bool w = true;
@@ -419,7 +427,8 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
         // visible columns of this half: lo <= c < lim (the lower bound only exists with a
         // token-exact window, on blocks outside the sink)
         const int key0 = (e >> 4) * BS + (BS == 128 ? 64 * hf : 0);
-        const int lim = ((e >> member) & 1) ? min(max(qi - key0 + 1, 0), 64) : 0;
+        int lim = ((e >> member) & 1) ? min(max(qi - key0 + 1, 0), 64) : 0;
+        if constexpr (kPaged) lim = (e >> 4) < a.ns ? min(lim, max(sink_end - key0, 0)) : lim;
         const int lo_abs = (a.exact_w > 0 && (e >> 4) >= a.ns) ? max(dstart, win_lo) : dstart;
         const int lo = min(max(lo_abs - key0, 0), 64);
 
@@ -475,9 +484,9 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
         // (an unset reference with every column masked gives zeros and stays unset; NaN compares false
         // and cannot appear: masked scores are -inf, whose exponential is 0)
         const bool look = unset ? (lim > lo) : !(psum <= a.max_prob);
-        // (kRefine: the halves that outweigh all before them are looked at too, with the same vote)
-        if (__any_sync(0xffffffffu, look || (kRefine && psum > l_run))) {
-          if (!kRefine || __any_sync(0xffffffffu, look)) {
+        // (kPaged: the halves that outweigh all before them are looked at too, with the same vote)
+        if (__any_sync(0xffffffffu, look || (kPaged && psum > l_run))) {
+          if (!kPaged || __any_sync(0xffffffffu, look)) {
             float mx = -INFINITY;
 #pragma unroll
             for (int c0 = 0; c0 < 64; c0 += C) {
@@ -496,7 +505,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
             const float m_new = fmaxf(m_ref, mx * a.scale_log2);
             const bool raise = look && m_new > m_ref;
             const float alpha = raise ? fast_exp2(m_ref - m_new) : 1.f;   // m_ref = -inf -> 0
-            if (raise) { m_ref = m_new; l_run *= alpha; if constexpr (kRefine) c_run *= alpha; }
+            if (raise) { m_ref = m_new; l_run *= alpha; if constexpr (kPaged) c_run *= alpha; }
             if (p0 + p1 > 0) {   // O already holds products: wait for them, then rescale my row
               ok = wait_o(13);
               if (!ok) break;
@@ -513,7 +522,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
             }
             exp_half((m_ref == -INFINITY) ? 0.f : -m_ref);
           }
-          if constexpr (kRefine) {
+          if constexpr (kPaged) {
             // A reference that stays behind the maximum costs nothing in fp32, but the largest probability of a row is then a rounded number
             // like the others, and where one key has most of the weight its rounding is the row's error.  It cancels when the row is
             // divided by the rounded probabilities' sum.  (Chunk of 1500 tokens, 64 / 8 heads, uneven keys: O is 1.50e-3 off in the norm, of which
@@ -548,8 +557,8 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
     if (ok && p0 + p1 > 0 && qi - lane < a.L && qi - lane + 32 > a.q_start) {
       const bool mine = qi < a.L && qi >= a.q_start;
       tc_fence_after();
-      const bool some = kRefine ? l_run != 0.f : l_run > 0.f;      // (kRefine: a sum that is NaN stays NaN)
-      const float inv_l = some ? 1.f / (kRefine ? l_run + c_run : l_run) : 0.f;
+      const bool some = kPaged ? l_run != 0.f : l_run > 0.f;      // (kPaged: a sum that is NaN stays NaN)
+      const float inv_l = some ? 1.f / (kPaged ? l_run + c_run : l_run) : 0.f;
       // rows leave through the slot's own Q tile (its last S product is done: it precedes the last P V in
       // the issuer's queue), 4 KB per warp, so that the stores cover whole rows (store_acc_64cols)
       uint8_t* stage = sQ + s * kTile + (warp & 3) * 4096;
@@ -582,7 +591,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
             uint32_t reg[32];
             tmem_ld32(my_o + c, reg);
             tmem_ld_wait();
-            if constexpr (kRefine) {                       // a piece's own quotient, weighed by its unrounded sum like the others'
+            if constexpr (kPaged) {                       // a piece's own quotient, weighed by its unrounded sum like the others'
               const float fit = l_run != 0.f ? l_run / (l_run + c_run) : 1.f;
 #pragma unroll
               for (int x = 0; x < 32; ++x) reg[x] = __float_as_uint(__uint_as_float(reg[x]) * fit);

@@ -9,6 +9,7 @@
 #include <atomic>
 
 #include "../../include/lg.h"
+#include "lg_paged.h"
 #include "lg_pattern.h"
 
 // Optional NVTX ranges around every entry point (build with -DLG_NVTX; the NVTX headers are
@@ -108,7 +109,12 @@ struct Resolved {          // validated, defaulted copy of lg_attn_params
   int kv_total;              // kv heads (times batch) of the whole problem: B * Hkv, more when the call works a group of its heads
   KvSplit split;             // how the dK/dV pass cuts its kv tiles (calls with a backward; see kv_split)
   FwdSplit fsplit;           // which super-tiles the forward cuts (see fwd_split)
-  bool late_reference;       // forward: the maxima of the rows are expected to rise often (see kFwdLateProb); 64-token blocks only
+  // forward of a chunk over the paged cache (null: another call): what each sequence holds; the maxima of the rows are expected to rise often
+  // (see kFwdLateProb); 64-token blocks only.  Tile lists of a sequence lie ent_stride entries and n_stiles ranks behind those of the one before
+  // (shared_lists: all sequences have the same)
+  const ChunkView* views;
+  int64_t ent_stride;
+  bool shared_lists;
 };
 
 // want_bwd: the call runs, prepares or sizes a backward; kv_total: kv heads of the whole problem when `p` is a group of

@@ -35,10 +35,6 @@ __device__ __forceinline__ void dequant16(uint4 c, float s, uint4& lo, uint4& hi
 
 constexpr int kGatherThreads = 256;
 
-// What a chunk attends to, as one sequence in time order: the `kept` tokens that the cache holds (the sink, then the ring from its
-// oldest token on, ring0 of the sequence), then the chunk's own rows.  One thread: 16 elements of K and of V, piece i of kv head h of
-// sequence b.  Rows whose page is absent are zeros, and so are those [sink, hidden) that no token of the chunk sees (a window edge that is
-// block-aligned): the weight of zero that they get does not silence a NaN.
 constexpr int kLineariseSeqs = 128;   // sequences of one launch
 struct PagedLinearise {
   const void* pool[2];       // K, V
@@ -47,9 +43,12 @@ struct PagedLinearise {
   void* lin[2];              // [B, Hkv, kept + T, D] bf16
   const int32_t* table;
   unsigned int* error_word;
-  int B, Hkv, D, T, kept, sink, hidden, window, page_shift, num_pages, stride;
-  int ring0[kLineariseSeqs]; // ring offset of each sequence's oldest kept token
+  int B, Hkv, D, T, kept, sink, window, page_shift, num_pages, stride;
+  ChunkSeq seq[kLineariseSeqs];
 };
+// One thread: 16 elements of K and of V, piece i of kv head h of sequence b.  Rows of the gap, rows whose page is absent and rows that no token
+// of the chunk sees are zeros: the weight of zero that they get does not silence a NaN.  Blocks of 64 that lie in the gap whole are on
+// no list and are not written.
 __device__ __forceinline__ void paged_linearise(const PagedLinearise& a, int64_t i, int h, int b) {
   const int row_shift = a.D == 128 ? 3 : 2, per_row = 1 << row_shift, L = a.kept + a.T;
   const int64_t v = i >> row_shift;
@@ -58,14 +57,19 @@ __device__ __forceinline__ void paged_linearise(const PagedLinearise& a, int64_t
   const int64_t bh = static_cast<int64_t>(b) * a.Hkv + h;
   uint4 lo[2], hi[2];
   if (v < a.kept) {
+    const ChunkSeq& s = a.seq[b];
+    const ChunkView view = chunk_view(a.kept, a.sink, s);
     int slot = static_cast<int>(v);
-    if (v >= a.sink) {
-      slot = a.ring0[b] + static_cast<int>(v) - a.sink;
+    if (!chunk_block_held(view, a.sink, slot >> 6)) return;
+    bool held = slot < view.sink_end;
+    if (slot >= a.sink) {
+      const int first = max(view.first, a.sink);
+      held = slot >= first && slot >= s.seen;
+      slot = s.ring0 + (held ? slot - first : 0);
       if (slot >= a.window) slot -= a.window;
       slot += a.sink;
     }
-    int page = checked_page(a.table[static_cast<int64_t>(b) * a.stride + (slot >> a.page_shift)], a.num_pages);
-    if (v >= a.sink && v < a.hidden) page = -1;
+    const int page = held ? checked_page(a.table[static_cast<int64_t>(b) * a.stride + (slot >> a.page_shift)], a.num_pages) : -1;
     const int64_t unit = (page < 0 ? 0 : page) * static_cast<int64_t>(a.Hkv) + h;
     const int64_t at = ((unit << a.page_shift) + (slot & ((1 << a.page_shift) - 1))) * per_row + c;
 #pragma unroll
@@ -90,11 +94,12 @@ __device__ __forceinline__ void paged_linearise(const PagedLinearise& a, int64_t
 }
 // Whether some entry that the kept tokens lie behind names no page; all threads of a block look.
 __device__ __forceinline__ bool paged_entry_missing(const PagedLinearise& a, int threads) {
-  const int pages = (a.kept + (1 << a.page_shift) - 1) >> a.page_shift;   // (a full ring, or its first slots)
+  const int round = (1 << a.page_shift) - 1, pages = (a.kept + round) >> a.page_shift;   // (at most: a full ring, or its first slots)
   bool missing = false;
   for (int64_t i = threadIdx.x; i < static_cast<int64_t>(a.B) * pages; i += threads) {
     const int64_t b = i / pages;
-    missing |= checked_page(a.table[b * a.stride + (i - b * pages)], a.num_pages) < 0;
+    const int page = static_cast<int>(i - b * pages);
+    if (page < (a.seq[b].held + round) >> a.page_shift) missing |= checked_page(a.table[b * a.stride + page], a.num_pages) < 0;
   }
   return __syncthreads_or(missing) != 0;
 }

@@ -100,4 +100,27 @@ __host__ __device__ __forceinline__ int page_exponent(uint32_t amax_bits /* of t
   return e < kPageMinExp ? kPageMinExp : e;
 }
 
+// What a chunk attends to, as one sequence in time order: `kept` rows with the tokens that the cache holds (the sink, then the ring from its
+// oldest token on), then the chunk's own rows.  A sequence that holds fewer than `kept` tokens has a gap between its sink and the rest (or
+// behind all it holds): distances, which the window goes by, are right behind the gap, and in the sink they do not count.
+struct ChunkSeq {
+  int held;                  // tokens that the cache holds
+  int ring0;                 // ring offset of the oldest token behind the sink
+  int phase;                 // position of a row behind the gap, less its row, modulo the window's block
+  int seen;                  // first row that the chunk's first token sees behind the sink
+};
+struct ChunkView {           // what the attention kernel asks of a sequence
+  int first;                 // first row behind the gap (0: no gap)
+  int sink_end;              // rows of the sink that hold a token
+  int phase, pad;
+};
+__host__ __device__ __forceinline__ ChunkView chunk_view(int kept, int sink, const ChunkSeq& s) {
+  if (s.held == kept) return ChunkView{0, sink, s.phase, 0};
+  return ChunkView{kept - (s.held > sink ? s.held - sink : 0), s.held < sink ? s.held : sink, s.phase, 0};
+}
+// Whether the 64 rows of block kb hold a row that a chunk may attend to.
+__host__ __device__ __forceinline__ bool chunk_block_held(const ChunkView& v, int sink, int kb) {
+  return kb * 64 < sink ? kb * 64 < v.sink_end : (kb + 1) * 64 > v.first;
+}
+
 }  // namespace lg

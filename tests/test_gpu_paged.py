@@ -474,6 +474,49 @@ def _check_chunk_rows(s, n, T, q, k, v, o, lse, rows, heads, weight=2.0 ** -8):
                 assert np.all(np.abs(np64(o[b, g, t]) - want) <= tol) and abs(lse[b, g, t].item() - l) <= tol_l, (b, g, t)
 
 
+RAGGED = [  # n, T, Hq, Hkv, D, sink, window, P, block: sequences that hold unequal numbers of tokens
+    ([0, 5, 63, 64, 65, 190, 1000], 70, 2, 1, 64, 64, 128, 16, 0),
+    ([0, 5, 63, 64, 65, 190, 1000], 65, 2, 1, 64, 64, 128, 32, 64),
+    ([1, 0, 7], 5, 2, 2, 128, 64, 64, 16, 0),                     # none has its sink
+    ([10, 100, 3, 400, 399], 200, 2, 1, 64, 64, 128, 64, 0),      # a chunk longer than the window, sinks that are not full
+    ([0, 300, 90, 1], 90, 2, 1, 128, 0, 256, 128, 0),             # no sink
+    ([130, 3000, 700, 129], 33, 2, 1, 128, 128, 2048, 64, 0),     # tiles cut along their keys, lists of unequal length
+    ([70, 2500, 300], 257, 8, 2, 64, 64, 1024, 16, 0),
+]
+
+
+@pytest.mark.parametrize("case", RAGGED, ids=lambda c: "B%d_T%d_D%d_W%d_%d" % (len(c[0]), c[1], c[4], c[6], c[8]))
+def test_chunk_of_sequences_at_their_own_positions(lg, case):
+    n, T, Hq, Hkv, D, sink, window, P, block = case
+    B = len(n)
+    s = Setup(lg, n, Hq, Hkv, D, sink, window, P, block=block)
+    for b, nb in enumerate(n):                                    # entries of pages without tokens are not read
+        s.ref.table[b, R.pages_of(nb, sink, window, P):] = -1
+    s.upload()
+    q, k, v = randn(B, Hq, T, D, seed=1), randn(B, Hkv, T, D, seed=2), randn(B, Hkv, T, D, seed=3)
+    ws = lg.paged_chunk_prefill_workspace(s.p, T, n)
+    ws[256:] = 255                                                # NaN wherever the call reads what it has not written
+    o, lse = lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n, workspace=ws)
+    assert lg.lg_last_status(ws) == 0
+    rows = sorted({0, 1, T // 3, T // 2, T - 2, T - 1} & set(range(T)))
+    _check_chunk_rows(s, n, T, q, k, v, o, lse, rows, range(0, Hq, max(1, Hq // 2)))
+    alone = [lg.lg_paged_chunk_prefill(lg.paged_params(1, Hq, Hkv, D, sink, window, page_tokens=P, num_pages=s.num_pages, block_tokens=block),
+                                       q[b:b + 1], k[b:b + 1], v[b:b + 1], *s.cache, s.table[b:b + 1], [n[b]]) for b in range(B)]
+    # every row against a call of its own: both are off by half a step of every weight and of o (2^-8 each), a score by 2^-19 scale sum |q k|
+    size = [max(x.float().abs().max().item(), (np.abs(R.decode_e4m3(c)).max(axis=(2, 3)) * sc).max())
+            for x, c, sc in zip((k, v), s.ref.codes, s.ref.scale)]
+    tol_l = 2 * 2.0 ** -19 / math.sqrt(D) * D * q.float().abs().max().item() * size[0] + 2.0 ** -16
+    for b in range(B):
+        want = alone[b][0][0].float()
+        assert ((o[b].float() - want).abs() <= 2 * (2.0 ** -8 + tol_l) * size[1] + 2 * 2.0 ** -8 * want.abs()).all()
+        assert (lse[b] - alone[b][1][0]).abs().max() <= tol_l
+    bad = next(b for b in range(B) if n[b] > 0)                   # an absent page of one sequence
+    s.ref.table[bad, 0] = s.num_pages
+    s.upload()
+    lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n, workspace=ws)
+    assert lg.lg_last_status(ws) == -7
+
+
 def test_chunk_of_more_rows_than_one_block_schedules(lg):
     T, n = 17000, [90]                                            # 67 super-tiles
     s = Setup(lg, n, 2, 1, 64, 0, 128, 64)

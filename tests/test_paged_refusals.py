@@ -90,13 +90,15 @@ def test_workspaces(lib):
     need = lib.lg_paged_decode_workspace_bytes(C.byref(p))
     assert need > 256
     assert _calls(lib, p, bytes=need - 1)["lg_paged_decode"] == WORKSPACE
-    n = (C.c_int64 * 2)(1000, 7)
-    need = lib.lg_paged_chunk_prefill_workspace_bytes(C.byref(p), 50, n)
-    assert need == max(lib.lg_paged_chunk_prefill_workspace_bytes(C.byref(_good(B=1)), 50, (C.c_int64 * 1)(x)) for x in (1000, 7))
-    assert _calls(lib, p, hn=n, T=50, bytes=need - 1)["lg_paged_chunk_prefill"] == WORKSPACE
-    # a batch at one position is one run, and so are full rings
-    one = lib.lg_paged_chunk_prefill_workspace_bytes(C.byref(_good(B=1)), 50, (C.c_int64 * 1)(1000))
-    assert lib.lg_paged_chunk_prefill_workspace_bytes(C.byref(p), 50, (C.c_int64 * 2)(1000, 2000)) > one
+    size = lambda T, *n: lib.lg_paged_chunk_prefill_workspace_bytes(C.byref(_good(B=len(n))), T, (C.c_int64 * len(n))(*n))
+    need = size(50, 1000, 7)
+    assert _calls(lib, p, hn=(C.c_int64 * 2)(1000, 7), T=50, bytes=need - 1)["lg_paged_chunk_prefill"] == WORKSPACE
+    # sequences at any positions are one run, as large as one of full rings
+    assert need == size(50, 1000, 2000) > size(50, 1000)
+    # but for a sink that is not full under a chunk longer than the window (256): runs of what holds equally many share the space
+    assert size(257, 1000, 7) == max(size(257, 1000), size(257, 7)) and size(257, 1000, 70) > size(257, 1000)
+    # and for chunks of more than 64 super-tiles
+    assert size(17000, 1000, 70) == max(size(17000, 1000), size(17000, 70))
 
 
 def test_chunk_limits(lib):

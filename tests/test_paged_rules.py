@@ -92,3 +92,71 @@ def test_reference_scale_is_the_smallest_that_covers():
         s = R.scale_for(np.array([0.0, -v, np.inf, np.nan]))
         assert v <= 448 * s and v > 224 * s
     assert R.scale_for(np.zeros(4)) == 1.0 and R.scale_for(np.array([np.nan])) == 1.0 and R.scale_for(np.array([1e-40])) == 2.0 ** -120
+
+
+CHUNK_SOURCE = r"""
+#define __forceinline__ inline
+#include "lg_paged.h"
+#include <cstdio>
+#include <cstdlib>
+using namespace lg;
+// The virtual sequence of a chunk (kept rows, then its own): which position a row stands for, and that what the attention kernel
+// derives from the rows is what the positions say.
+int main() {
+  std::srand(5);
+  int gaps = 0, short_sinks = 0;
+  for (int i = 0; i < 3000; ++i) {
+    const int sink = 64 * (std::rand() % 3), block = std::rand() % 2 ? 0 : (std::rand() % 2 ? 64 : 16), window = 64 * (1 + std::rand() % 4);
+    const int cap = sink + window, T = 1 + std::rand() % (block ? window - block + 1 : window);      // (no more than a sequence without its sink allows)
+    const int64_t n = std::rand() % 4 == 0 ? std::rand() % (sink + 1) : std::rand() % 1500;
+    const int held = n < cap ? n : cap;
+    int kept = held;
+    if (held < cap && std::rand() % 4) { kept = held + std::rand() % (cap - held + 1); if (kept != held && kept < sink) kept = sink; }
+    ChunkSeq s;
+    s.held = held;
+    s.ring0 = (n - held) % window;
+    s.phase = block ? (((n - kept) % block) + block) % block : 0;
+    s.seen = 0;
+    const ChunkView view = chunk_view(kept, sink, s);
+    gaps += kept > held; short_sinks += kept > held && held < sink;
+    const int first = view.first > sink ? view.first : sink;
+    int found = 0;
+    for (int v = 0; v < kept + T; ++v) {
+      // the position that row v holds (-1: none)
+      int64_t pos = -1;
+      if (v >= kept) pos = n + v - kept;
+      else if (v < sink) pos = v < view.sink_end ? v : -1;
+      else if (v >= first) pos = n - (kept - v);
+      if (pos >= 0 && v < kept) {
+        ++found;
+        if (pos >= n || (v >= sink && (pos < sink || slot_of(pos, sink, window) != sink + (s.ring0 + v - first) % window))) { std::printf("row %d\n", v); return 1; }
+        if (!chunk_block_held(view, sink, v / 64)) { std::printf("block %d\n", v / 64); return 1; }
+      }
+      for (int t = 0; t < T; t += 1 + T / 7) {
+        const int q = kept + t;
+        const int64_t at = n + t;
+        const int lo0 = block ? ((q + s.phase) / block - window / block + 1) * block - s.phase : q - window + 1;
+        const int lo = v < sink ? 0 : (lo0 > view.first ? lo0 : view.first), end = v < sink && view.sink_end < q + 1 ? view.sink_end : q + 1;
+        const bool kernel = v >= lo && v < end;
+        const bool near = block ? at / block - pos / block < window / block : at - pos < window;
+        const bool want = pos >= 0 && pos <= at && (near || pos < sink);
+        if (kernel != want) { std::printf("row %d of query %d: %d, sink %d window %d block %d n %d kept %d\n", v, t, kernel, sink, window, block, (int)n, kept); return 1; }
+      }
+    }
+    if (found != held && !(kept == held && held < sink)) { std::printf("held %d of %d\n", found, held); return 1; }
+  }
+  std::printf(gaps > 500 && short_sinks > 100 ? "ok\n" : "few\n");
+  return 0;
+}
+"""
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs a host compiler")
+def test_rows_of_a_chunk_against_positions(tmp_path):
+    src, exe = tmp_path / "t.cpp", tmp_path / "t"
+    src.write_text(CHUNK_SOURCE)
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-I", build.CSRC, "-I", os.path.join(cuda, "include"), str(src), "-o",
+                    str(exe)], check=True)
+    out = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert out.stdout.split() == ["ok"] and out.returncode == 0, out.stdout
