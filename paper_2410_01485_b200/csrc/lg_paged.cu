@@ -397,8 +397,8 @@ __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const Gath
 }
 
 // ---- single-token attention ---------------------------------------------------------------------
-// The 32-token tiles of all (sequence, kv head, group of <= 8 query heads) units form one sequence that is cut into equal
-// runs, one per warp (a CTA's warps have neighbouring runs).  A warp streams its run through a ring of its own of
+// The 32-token tiles of all (sequence, kv head, group of <= 8 query heads) units form one sequence that is cut into slices, one per CTA
+// (kMergeTiles), and these into equal runs, one per warp.  A warp streams its run through a ring of its own of
 // kPagedSlots half tiles, K and V in turn (cp.async, 16-byte pieces XOR-swizzled by the row, so that fragments are read without
 // bank conflicts); the ring runs on from one unit to the next, so the latencies of a unit (its pages, its scales, its tiles) are
 // paid behind the tiles of the one before.  A unit that lies inside a run is finished by its warp; of the others a warp has
@@ -419,6 +419,14 @@ constexpr int kPagedTile = 32, kPagedHalf = 16;   // tokens of a tile, and of wh
 constexpr int kPagedSlots = 5;          // 4 KB each at D = 128: three tiles' K and two tiles' V, or the other way round
 constexpr int kPagedMaxB = 4096;        // sequences of one launch (their prefix sums lie in shared memory)
 constexpr int kPagedMaxCtas = 320;
+// Slices that cut across units make some CTA merge the records of two of them, one after the other, and wait twice: about what this many tiles of
+// a CTA take.  So a CTA gets a unit whole, or an equal share of one, unless the longest unit is so far above the average slice that the idle
+// CTAs cost more.  Decode and append, cut evenly across units | kept to them:
+//   several CTAs a unit        1 sequence x 8 kv heads x 4224 slots 12.4 | 11.2 us, 1 x 4 x 8192 13.6 | 11.2, 4 x 4 x 4096 13.6 | 12.0, 8 x 2 x 1088 (D = 64) 9.3 | 8.2
+//   one (longest / average)    16 x 8 x 4224 (1.16) 33.8 | 31.6, 14 x 8 x 2048 (64 tiles, 1.32) 19.8 | 18.1, 10 x 8 x 1024 (1.85) 14.9 | 13.0, 48 x 4 x 1088 (D = 64, 1.54) 15.7 | 13.2;
+//                              but 14 x 8 x 8320 (260 tiles, 1.32) 49.1 | 51.1, 10 x 8 x 4224 (1.85) 23.8 | 30.4
+//   several units, alike, a CTA   32 x 8 x 4224 58.4 | 56.1, 200 x 8 x 1024 94.2 | 90.3
+constexpr uint32_t kMergeTiles = 16;
 constexpr float kNoScore = -3.4e38f;    // the reference of a row that has attended nothing
 
 struct PagedDecodeArgs {
@@ -674,13 +682,50 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
     per = max(1u, (total + gridDim.x - 1) / gridDim.x);
     f0 = min(total, per * me);
     f1 = min(total, f0 + per);
+    int mates = 0, ahead = 0;                                           // CTAs that share my only unit, those of them before me (0: slices across units)
+    // slices that keep to units (kMergeTiles)
+    if (a.B <= 2 * kSms) {
+      const uint32_t grid = gridDim.x, units = ups * a.B, all = cum[a.B];
+      auto tiles_of = [&](int b) { return b < a.B ? static_cast<uint32_t>(cum[b + 1] - cum[b]) : 0u; };
+      uint32_t most = 0, cut = 0;
+#pragma unroll 1
+      for (int b = lane; b < a.B; b += 32) most = max(most, tiles_of(b));
+      most = __reduce_max_sync(0xffffffffu, most);
+      const uint32_t held = (units + grid - 1) / grid * most;
+      if (2 * units <= grid) cut = (all + grid / ups - a.B - 1) / (grid / ups - a.B);   // several CTAs a unit: that many fit whatever the lengths
+      else if (held <= max(per + kMergeTiles, per + per / 5)) {
+        if (units <= grid) cut = most;                                                // one a unit
+        else if (most * a.B == all) { per = held; f0 = min(total, per * me); f1 = min(total, f0 + per); }   // several units, alike, a CTA
+      }
+      if (cut > 0) {
+        f0 = f1 = total;
+        uint32_t before = 0;                                            // CTAs of the sequences before b0
+#pragma unroll 1
+        for (int b0 = 0; b0 < a.B; b0 += 32) {                          // (a lane per sequence)
+          const uint32_t nt = tiles_of(b0 + lane), n = (nt + cut - 1) / cut;
+          uint32_t upto = n * ups;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) { const uint32_t t = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += t; }
+          upto += before;
+          const unsigned past = __ballot_sync(0xffffffffu, upto > static_cast<uint32_t>(me));
+          if (past == 0) { before = __shfl_sync(0xffffffffu, upto, 31); continue; }
+          const int y = __ffs(past) - 1;
+          const uint32_t nb = __shfl_sync(0xffffffffu, n, y), ntb = __shfl_sync(0xffffffffu, nt, y), at = me - (__shfl_sync(0xffffffffu, upto, y) - nb * ups);
+          const uint32_t k = at / nb, each = ntb / nb, more = ntb - each * nb;   // (the first `more` CTAs of a unit take one tile more)
+          mates = nb; ahead = at - k * nb;
+          f0 = static_cast<uint32_t>(cum[b0 + y]) * ups + k * ntb + ahead * each + min(static_cast<uint32_t>(ahead), more);
+          f1 = f0 + each + (static_cast<uint32_t>(ahead) < more ? 1 : 0);
+          break;
+        }
+      }
+    }
     g0 = f0 + (f1 - f0) * warp / kDecWarps;
     g1 = f0 + (f1 - f0) * (warp + 1) / kDecWarps;
     if (g0 < g1) { next.at = find(g0); fetch(next, g1 - g0); }
     if (warp < 2 && f0 < f1) {                                          // who shares my CTA's first (warp 0) and last unit
       const TilePos p = find(warp ? f1 - 1 : f0);
       const uint32_t k = p.kvh * a.HG + p.hg, first = static_cast<uint32_t>(cum[p.b]) * ups + k * p.nt;
-      const int c_lo = static_cast<int>(first / per), c_hi = static_cast<int>((first + p.nt - 1) / per);
+      const int c_lo = mates > 0 ? me - ahead : static_cast<int>(first / per), c_hi = mates > 0 ? c_lo + mates - 1 : static_cast<int>((first + p.nt - 1) / per);
       if (lane == 0) {
         reinterpret_cast<int4*>(sm + SM::kShare)[2 * warp] = make_int4(p.b * ups + k, c_lo, c_hi - c_lo + 1, p.b * a.Hq + p.kvh * a.G + p.hg * kDecHeads);
         reinterpret_cast<int4*>(sm + SM::kShare)[2 * warp + 1].x = min(kDecHeads, a.G - p.hg * kDecHeads);
@@ -1139,7 +1184,7 @@ lg_status check_paged(const lg_paged_params* p) {
   if (p->D != 64 && p->D != 128) return LG_ERR_UNSUPPORTED;
   if (static_cast<int64_t>(p->sink_tokens) + p->window_tokens > (1ll << 30)) return LG_ERR_UNSUPPORTED;
   if (p->table_stride > 0 && p->table_stride < table_columns(p)) return LG_ERR_INVALID_ARG;
-  // rows of a pool are addressed by TMA coordinates of 32 bits
+  // the decode numbers the rows of a pool in 32 bits
   if (static_cast<int64_t>(p->num_pages) * p->Hkv * p->page_tokens > 0x7fffffffll) return LG_ERR_UNSUPPORTED;
   return LG_OK;
 }

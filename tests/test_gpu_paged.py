@@ -279,6 +279,30 @@ def test_decode(lg, case):
     assert none is None and torch.equal(o, only)
 
 
+SLICES = [  # n, Hq, Hkv, D, window, P: how units (sequence, kv head) and CTAs share each other
+    ([900, 0, 33, 2000], 8, 1, 128, 2048, 16),                    # several CTAs a unit, of unequal lengths
+    ([0, 0, 1, 5000], 6, 3, 64, 4096, 64),
+    ([500 + b if b % 9 else 0 for b in range(40)], 8, 4, 64, 512, 32),   # one CTA a unit, sequences beyond the first 32
+    ([97 + b % 31 for b in range(40)], 8, 8, 128, 128, 16),       # three units a CTA, all of four tiles
+    ([97] * 39 + [96], 8, 8, 128, 128, 16),                       # ... and one of three
+    ([8000] + [10] * 20, 4, 4, 128, 8192, 128),                   # across units: one of them is far longer than the rest
+    ([300] * 299, 1, 1, 64, 288, 32),                             # more sequences than are looked at
+]
+
+
+@pytest.mark.parametrize("case", SLICES, ids=lambda c: "B%d_%d_%d_D%d_W%d" % (len(c[0]), c[1], c[2], c[3], c[4]))
+def test_decode_slices(lg, case):
+    n, Hq, Hkv, D, window, P = case
+    s = Setup(lg, n, Hq, Hkv, D, 0, window, P)
+    q = randn(len(n), Hq, D, seed=3)
+    ws = lg.paged_decode_workspace(s.p)
+    ws[256 + 4 * len(n) * Hkv + 256:] = 255                       # records that are read have been written
+    o, lse = lg.lg_paged_decode(s.p, q, *s.cache, s.table, s.counts(), workspace=ws)
+    s.check_decode(q, o, lse)
+    again, lse2 = lg.lg_paged_decode(s.p, q, *s.cache, s.table, s.counts(), workspace=ws)
+    assert torch.equal(o, again) and torch.equal(lse, lse2) and lg.lg_last_status(ws) == 0
+
+
 @pytest.mark.parametrize("D, P, block", [(128, 16, 0), (64, 64, 32), (128, 32, 32)])
 def test_decode_reads_nothing_it_does_not_attend(lg, D, P, block):
     """NaN codes and NaN scales in empty slots, in pages of nobody, and in ring tokens that the block-aligned window leaves out."""
