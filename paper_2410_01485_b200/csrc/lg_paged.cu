@@ -902,7 +902,6 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
 
     // ---- S^T[32 tokens, 8 heads] = K Q^T
     float s[2][4] = {};
-    // ---- S^T[32 tokens, 8 heads] = K Q^T
     const uint32_t sk = ring + slot;
 #pragma unroll
     for (int k = 0; k < D / 16; k += 2) {
