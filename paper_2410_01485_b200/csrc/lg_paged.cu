@@ -410,8 +410,8 @@ __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const Gath
 // (K as e4m3 in products of its own kind, with q as the sum of two e4m3 numbers, needs no conversion but was slower: one sequence over 4224
 // slots 14.0 us against 12.4 with its append, 16 over 60-131 thousand 531 us against 500.)
 // A page's K scale multiplies its scores; that of V goes into the weights, w_j = p_j vs / vs_ref with the largest scale of the unit so far, so that
-// they fit f16 (11 bits), while the row sum is kept in fp32.  Where the scales of a unit's pages lie more than 2^10 apart that would cost
-// bits, and the weights get a running reference of their own, w_j = 2^(s_j + log2 vs - r).
+// they fit f16 (11 bits down to 2^-14), while the row sum is kept in fp32.  Where the scales of a unit's pages lie more than 2^6 apart that would
+// cost bits, and the weights get a running reference of their own, w_j = 2^(s_j + log2 vs - r).
 // The instructions of a tile count although HBM bounds the kernel: in a loop of milliseconds the board is at its power limit, and the clock
 // that it takes back is the SMs' (16 sequences over 60-131 thousand slots, 600 steps in a row: 521 us with a maximum and a rescaling in every
 // tile and two exponentials a weight, 500 us so).
@@ -956,6 +956,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
       }
     };
     float be0 = 1.f, be1 = 1.f;               // what O is multiplied by
+    const float was0 = m_run[0], was1 = m_run[1];
     bool moved = false;
     scores(m_run[0], m_run[1]);
     top();
@@ -982,10 +983,11 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
     if (!own && v0 > 0.f && (fmaxf(v0, v1) > vs_ref || fminf(v0, v1) < vs_min)) {
       const float most = fmaxf(vs_ref, fmaxf(v0, v1));
       vs_min = fminf(vs_min, fminf(v0, v1));
-      own = vs_min * 1024.f < most;           // (then O keeps the reference that it has)
-      if (own) {
+      own = vs_min * 64.f < most;
+      if (own) {                              // O keeps the reference that it had: what moved m may weigh little, having a small scale
         const float lr = fast_log2(vs_ref);
-        r_run[0] = vs_ref > 0.f ? m_run[0] + lr : kNoScore; r_run[1] = vs_ref > 0.f ? m_run[1] + lr : kNoScore;
+        r_run[0] = vs_ref > 0.f ? was0 + lr : kNoScore; r_run[1] = vs_ref > 0.f ? was1 + lr : kNoScore;
+        be0 = be1 = 1.f;
       } else if (most != vs_ref) {
         if (vs_ref > 0.f) { be0 *= vs_ref / most; be1 *= vs_ref / most; moved = true; }
         vs_inv = 1.f / most;

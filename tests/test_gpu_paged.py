@@ -346,6 +346,18 @@ def test_decode_pages_of_far_apart_scales(lg, P, D):
     s.check_decode(20 * q, o, lse)
 
 
+@pytest.mark.parametrize("P, D, spread, size", [(32, 64, 40, 20), (16, 128, 40, 20), (64, 64, 5, 5), (128, 128, 3, 5), (32, 64, 8, 20)])
+def test_decode_long_runs_over_scales_and_scores_far_apart(lg, P, D, spread, size):
+    """A warp works several tiles, whose scores and V scales rise and fall past each other."""
+    n = [1024 - 7 * b for b in range(40)]
+    s = Setup(lg, n, 4, 4, D, 0, 1024, P, scales=(-spread, spread))
+    s.ref.scale[0][:] = 2.0 ** np.random.RandomState(1).randint(-9, -5, s.ref.scale[0].shape)
+    s.upload()
+    q = size * randn(40, 4, D, seed=5)
+    o, lse = lg.lg_paged_decode(s.p, q, *s.cache, s.table, s.counts())
+    s.check_decode(q, o, lse)
+
+
 @pytest.mark.parametrize("m", [2.0 ** -100, 2.0 ** 60, 0.0])
 def test_decode_q_of_any_size(lg, m):
     s = Setup(lg, [100, 300], 4, 1, 128, 0, 512, 32)
