@@ -419,13 +419,13 @@ constexpr int kPagedTile = 32, kPagedHalf = 16;   // tokens of a tile, and of wh
 constexpr int kPagedSlots = 5;          // 4 KB each at D = 128: three tiles' K and two tiles' V, or the other way round
 constexpr int kPagedMaxB = 4096;        // sequences of one launch (their prefix sums lie in shared memory)
 constexpr int kPagedMaxCtas = 320;
-// Slices that cut across units make some CTA merge the records of two of them, one after the other, and wait twice: about what this many tiles of
-// a CTA take.  So a CTA gets a unit whole, or an equal share of one, unless the longest unit is so far above the average slice that the idle
-// CTAs cost more.  Decode and append, cut evenly across units | kept to them:
-//   several CTAs a unit        1 sequence x 8 kv heads x 4224 slots 12.4 | 11.2 us, 1 x 4 x 8192 13.6 | 11.2, 4 x 4 x 4096 13.6 | 12.0, 8 x 2 x 1088 (D = 64) 9.3 | 8.2
-//   one (longest / average)    16 x 8 x 4224 (1.16) 33.8 | 31.6, 14 x 8 x 2048 (64 tiles, 1.32) 19.8 | 18.1, 10 x 8 x 1024 (1.85) 14.9 | 13.0, 48 x 4 x 1088 (D = 64, 1.54) 15.7 | 13.2;
-//                              but 14 x 8 x 8320 (260 tiles, 1.32) 49.1 | 51.1, 10 x 8 x 4224 (1.85) 23.8 | 30.4
-//   several units, alike, a CTA   32 x 8 x 4224 58.4 | 56.1, 200 x 8 x 1024 94.2 | 90.3
+// Slices that cut across units make some CTA merge the records of two of them, one after the other, and wait twice: about what kMergeTiles
+// tiles of a CTA take, half of that where units are still shared by several CTAs of their own.  So a CTA gets a unit whole, or an equal share of
+// one, where the largest share is at most that, or a fifth, above the average one.  Decode and append, cut evenly across units | so:
+//   one CTA a unit      16 sequences x 8 kv heads x 4224 slots 33.7 | 31.5 us, 14 x 8 x 1024 16.0 | 13.2, 48 x 4 x 1088 (D = 64) 15.6 | 13.2, 24 x 8 x 512 (D = 64)
+//                       13.6 | 9.7 (10 x 8 x 4224, where the share is 132 tiles and the average 72, would be 23.8 | 30.4, and is cut evenly)
+//   several             1 x 8 x 4224 12.4 | 11.2, 1 x 4 x 8192 13.6 | 11.2, 4 x 8 x 4224 16.3 | 15.2, 9 x 8 x 4224 22.5 | 21.3
+//   several units a CTA, if alike   32 x 8 x 4224 58.4 | 56.1, 200 x 8 x 1024 94.2 | 90.3
 constexpr uint32_t kMergeTiles = 16;
 constexpr float kNoScore = -3.4e38f;    // the reference of a row that has attended nothing
 
@@ -692,10 +692,25 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
       for (int b = lane; b < a.B; b += 32) most = max(most, tiles_of(b));
       most = __reduce_max_sync(0xffffffffu, most);
       const uint32_t held = (units + grid - 1) / grid * most;
-      if (2 * units <= grid) cut = (all + grid / ups - a.B - 1) / (grid / ups - a.B);   // several CTAs a unit: that many fit whatever the lengths
-      else if (held <= max(per + kMergeTiles, per + per / 5)) {
-        if (units <= grid) cut = most;                                                // one a unit
-        else if (most * a.B == all) { per = held; f0 = min(total, per * me); f1 = min(total, f0 + per); }   // several units, alike, a CTA
+      if (held <= max(per + kMergeTiles, per + per / 5)) {              // units whole
+        if (units <= grid) cut = most;
+        else if (most * a.B == all) { per = held; f0 = min(total, per * me); f1 = min(total, f0 + per); }   // (several a CTA: alike ones only)
+      } else if (2 * units <= grid) {                                   // several CTAs a unit: shares of up to `cut` tiles, as small as all fit
+        const uint32_t slices = grid / ups, room = max(per + kMergeTiles / 2, per + per / 5);   // (of a kv head's units together)
+        cut = (all + slices - 1) / slices;
+#pragma unroll 1
+        for (int tries = 0; cut <= room; ++tries) {
+          uint32_t sum = 0, next_cut = most;                            // CTAs; the smallest cut with which a unit takes one less
+#pragma unroll 1
+          for (int b = lane; b < a.B; b += 32) {
+            const uint32_t nt = tiles_of(b), n = (nt + cut - 1) / cut;
+            sum += n;
+            if (n > 1) next_cut = min(next_cut, (nt + n - 2) / (n - 1));
+          }
+          if (__reduce_add_sync(0xffffffffu, sum) <= slices) break;
+          cut = tries < 8 ? max(__reduce_min_sync(0xffffffffu, next_cut), cut + cut / 32) : most;
+        }
+        if (cut > room) cut = 0;
       }
       if (cut > 0) {
         f0 = f1 = total;
