@@ -434,13 +434,14 @@ lg_status lg_paged_decode(const lg_paged_params* p, const void* q, const void* k
 /* lg_chunk_prefill over the paged cache: T new tokens of every sequence attend to what its cache holds and, causally, to
  * themselves (the chunk's own k_chunk, v_chunk as given, in bf16: they are rounded when they are appended, afterwards, by
  * lg_paged_append).  n_tokens_before: HOST int64 [B], >= 0 each, any of them beside any other.  (Sequences at unequal
- * positions are worked together but for a chunk of more than 16000 tokens, and for one longer than the window beside a
- * sequence that holds fewer than sink_tokens: neighbours that hold equally many should then stand side by side.)
+ * positions are worked together but for a chunk of more than 16000 tokens, and for one longer than the window (than all
+ * but one token of its last block, where the window is block-aligned) beside a sequence that holds fewer than sink_tokens:
+ * sequences that hold equally many should then be neighbours.)
  * sink_tokens and window_tokens are multiples of 64, window_tokens >= 64.  The cache is copied in bf16 and in time order
  * into the workspace (device, 256-byte aligned,
  * lg_paged_chunk_prefill_workspace_bytes() bytes), and the forward kernel runs over it.  As there, a V that is not finite
  * reaches every query whose tile holds its token, whether the query sees it or not (tokens that no query of the chunk sees
- * are left out).  A failure of any of the launches is reported by lg_last_status(workspace, stream).                                                         */
+ * are left out).  A failure of any of the launches is reported by lg_last_status(workspace, stream).                   */
 size_t lg_paged_chunk_prefill_workspace_bytes(const lg_paged_params* p, int32_t T, const int64_t* n_tokens_before);
 lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, const void* k_chunk,
                                  const void* v_chunk, const void* k_pool, const void* v_pool, const float* k_scale,
