@@ -563,6 +563,29 @@ def test_chunk_of_more_rows_than_one_block_schedules(lg):
     _check_chunk_rows(s, n, T, q, k, v, o, lse, [0, 1, 37, 38, 255, 256, 9999, 16639, 16640, T - 1], [0, 1])
 
 
+def test_chunk_of_many_rows_at_two_phases(lg):
+    """One schedule for all sequences, which hold as many tokens but whose window's blocks lie differently."""
+    T, n = 16400, [1000, 1030]                                    # 65 super-tiles
+    s = Setup(lg, n, 1, 1, 64, 64, 128, 64, block=64)
+    q, k, v = randn(2, 1, T, 64, seed=1), randn(2, 1, T, 64, seed=2), randn(2, 1, T, 64, seed=3)
+    ws = lg.paged_chunk_prefill_workspace(s.p, T, n)
+    o, lse = lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n, workspace=ws)
+    assert lg.lg_last_status(ws) == 0
+    _check_chunk_rows(s, n, T, q, k, v, o, lse, [0, 1, 23, 24, 25, 127, 128, 9999, T - 1], [0])
+
+
+def test_chunk_of_two_tiles_an_sm_over_gaps(lg):
+    """D = 64 on a grid whose CTAs share SMs, sequences that hold unequal numbers of tokens."""
+    T, n = 300, [0, 31, 64, 100, 200, 319, 320, 5000]
+    s = Setup(lg, n, 16, 4, 64, 64, 256, 32)
+    q, k, v = randn(8, 16, T, 64, seed=1), randn(8, 4, T, 64, seed=2), randn(8, 4, T, 64, seed=3)
+    ws = lg.paged_chunk_prefill_workspace(s.p, T, n)
+    ws[256:] = 255
+    o, lse = lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n, workspace=ws)
+    assert lg.lg_last_status(ws) == 0
+    _check_chunk_rows(s, n, T, q, k, v, o, lse, [0, 1, 63, 64, 127, 128, 255, 256, 299], [0, 7, 15])
+
+
 def test_chunk_of_more_sequences_than_one_launch(lg):
     B, T = 133, 3
     n = [70 + b for b in range(B)]                                # full rings: one run of neighbours, each at its own offset
