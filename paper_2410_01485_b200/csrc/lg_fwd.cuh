@@ -154,7 +154,8 @@ __device__ __forceinline__ void fwd_join(const FwdArgs& a, uint32_t base, uint32
   else fwd_join_rows<D, 8, 2>(a, base, n_segs, b, h, row0, first, end, step, c);
 }
 
-// kPaged: a chunk over the paged cache.  Its sequences have their own lists and views, and O is divided by the sum of the probabilities as they were rounded to bf16 where they weigh, the LSE by that of the unrounded ones (below).
+// kPaged: a chunk over the paged cache.  Its sequences have their own lists and views, and O is divided by the sum of the probabilities as they
+// were rounded to bf16 where they weigh, the LSE goes by that of the unrounded ones (below).
 template <int D, int BS, int NB /* score buffers per slot */, bool kSplit, bool kPaged = false>
 __global__ void __launch_bounds__(kFwdThreads, fwd_ctas_per_sm(NB))
 fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
