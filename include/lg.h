@@ -423,8 +423,8 @@ lg_status lg_paged_gather(const lg_paged_params* p, const void* k_pool, const vo
  * int64 [B]) counts the tokens appended so far, the current one included.  Scores and outputs are computed from the codes
  * without further rounding of K, V or q (but for elements of a row of q below 2^-24 of its largest); the weights are
  * rounded to f16, their sum is not.  workspace: device, 256-byte aligned, lg_paged_decode_workspace_bytes() bytes (0 = invalid
- * arguments), zero-filled once by lg_sparse_decode_workspace_init(); two calls that can run at the same time (two captured
- * graphs too) need a workspace each.                                                                                 */
+ * arguments), zero-filled once by lg_sparse_decode_workspace_init(); one that is large enough for several calls serves them in
+ * turn, whatever their sizes; two calls that can run at the same time (two captured graphs too) need a workspace each.   */
 size_t lg_paged_decode_workspace_bytes(const lg_paged_params* p);
 lg_status lg_paged_decode(const lg_paged_params* p, const void* q, const void* k_pool, const void* v_pool,
                           const float* k_scale, const float* v_scale, const int32_t* block_table,

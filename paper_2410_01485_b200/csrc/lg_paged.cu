@@ -418,7 +418,6 @@ __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const Gath
 constexpr int kPagedTile = 32, kPagedHalf = 16;   // tokens of a tile, and of what lies in one page whatever its size
 constexpr int kPagedSlots = 5;          // 4 KB each at D = 128: three tiles' K and two tiles' V, or the other way round
 constexpr int kPagedMaxB = 4096;        // sequences of one launch (their prefix sums lie in shared memory)
-constexpr int kPagedMaxCtas = 320;
 // Slices that cut across units make some CTA merge the records of two of them, one after the other, and wait twice: about what kMergeTiles
 // tiles of a CTA take, half of that where units are still shared by several CTAs of their own.  So a CTA gets a unit whole, or an equal share of
 // one, where the largest share is at most that, or a fifth, above the average one.  Decode and append, cut evenly across units | so:
@@ -1167,8 +1166,9 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
     const int4 sh = threadIdx.x ? sh1 : sh0;
     bool last = false;
     if (sh.z > 1 && (threadIdx.x == 0 || sh1.x != sh0.x)) {
-      last = ticket_add(a.unit_count + sh.x) + 1u == static_cast<unsigned>(sh.z);
-      if (last) a.unit_count[sh.x] = 0u;
+      unsigned int* count = unit_counter(a.unit_count, a.B * ups, sh.x, sh.y);
+      last = ticket_add(count) + 1u == static_cast<unsigned>(sh.z);
+      if (last) *count = 0u;
     }
     s_last[threadIdx.x] = last;
   }
@@ -1241,20 +1241,18 @@ static lg_status allow_decode_smem() {
   return LG_OK;
 }
 
-struct PagedDecodePlan { int HG, slice, n_cta; int64_t units; size_t count_bytes, total_bytes; };
+struct PagedDecodePlan { int HG, slice, n_cta; int64_t units; size_t total_bytes; };
 static PagedDecodePlan plan_paged_decode(const lg_paged_params* p) {
   PagedDecodePlan w;
   w.HG = (p->Hq / p->Hkv + kDecHeads - 1) / kDecHeads;
   // sequences of one launch: their prefix sums lie in shared memory, and the kernel counts their tiles in 31 bits
   const int64_t C = static_cast<int64_t>(p->sink_tokens) + p->window_tokens, seq_units = static_cast<int64_t>(p->Hkv) * w.HG;
   const int64_t seq_tiles = seq_units * ((C + kPagedTile - 1) / kPagedTile);
-  int64_t most_b = 0x7fffffffll / (seq_tiles + kPagedMaxCtas);
+  int64_t most_b = 0x7fffffffll / (seq_tiles + kDecMaxCtas);
   if (most_b > kPagedMaxB) most_b = kPagedMaxB;
   w.slice = static_cast<int>(p->B < most_b ? p->B : most_b);      // (0: one sequence is too long)
   w.units = w.slice * seq_units;
-  w.count_bytes = align_up(static_cast<size_t>(w.units) * sizeof(unsigned int), 256);
-  w.total_bytes = sizeof(WsHeader) + w.count_bytes +
-                  align_up((static_cast<size_t>(kPagedMaxCtas) + w.units) * kDecHeads * (p->D + 2) * sizeof(float), 256);
+  w.total_bytes = kDecRecordOffset + align_up((static_cast<size_t>(kDecMaxCtas) + w.units) * kDecHeads * (p->D + 2) * sizeof(float), 256);
   // as many CTAs as fit an SM (D = 64: two), each with at least a tile for every second of its warps
   const int64_t tiles = w.slice * seq_tiles;
   int64_t n = (tiles + kDecWarps / 2 - 1) / (kDecWarps / 2);
@@ -1422,8 +1420,8 @@ lg_status lg_paged_decode(const lg_paged_params* p, const void* q, const void* k
   a.pool[0] = static_cast<const uint8_t*>(k_pool); a.pool[1] = static_cast<const uint8_t*>(v_pool);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   a.error_word = reinterpret_cast<unsigned int*>(ws);
-  a.unit_count = reinterpret_cast<unsigned int*>(ws + sizeof(WsHeader));
-  a.part = reinterpret_cast<float*>(ws + sizeof(WsHeader) + w.count_bytes);
+  a.unit_count = reinterpret_cast<unsigned int*>(ws + kDecCountOffset);
+  a.part = reinterpret_cast<float*>(ws + kDecRecordOffset);
   a.Hq = p->Hq; a.Hkv = p->Hkv; a.G = p->Hq / p->Hkv; a.HG = w.HG;
   a.C = p->sink_tokens + p->window_tokens;
   a.sink = p->sink_tokens; a.block_tokens = p->block_tokens;
