@@ -259,9 +259,10 @@ size_t lg_sparse_decode_workspace_bytes(const lg_decode_params* p);
 
 /* A decode workspace must be zero-filled once before its first use (this call, or any memset);
  * every lg_sparse_decode call leaves it ready for the next one, so a serving loop pays no
- * clearing per token.  (The first bytes hold the status word and one arrival counter per
- * (sequence, kv head, head group); the CTA that completes a unit resets its counter.)  Call it
- * again after a launch that failed.                                                       */
+ * clearing per token.  (The first 1536 bytes hold the status word and arrival counters, at places
+ * that no sizes move; the CTA that completes a unit resets its counter.)  A workspace that is
+ * large enough for several calls serves them in turn, whatever their sizes.  Call it again
+ * after a launch that failed.                                                             */
 lg_status lg_sparse_decode_workspace_init(void* workspace, size_t workspace_bytes, void* stream);
 
 /* One query token per sequence attends to every valid slot of its cache:

@@ -39,7 +39,7 @@ struct DecodeArgs {
   float scale_log2;
   int sink, block_tokens;        // sink slots; block of the block-aligned window (0: every held token is attended)
   int B;                         // sequences (flattened path)
-  unsigned int* unit_count;      // [B * Hkv * HG] records delivered per unit (flattened path; zero between calls)
+  unsigned int* unit_count;      // [kDecMaxCtas] records delivered per unit (flattened path; unit_counter, zero between calls)
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t smem_addr, const void* gptr, bool valid) {
@@ -299,7 +299,6 @@ __global__ void __launch_bounds__(kDecWarps * 32) decode_split_kernel(const Deco
 // covers the whole cache.  A slice that crosses a unit boundary is processed in segments; the
 // record of (CTA c, unit u) lives at index c + u, which grows strictly along the sequence.
 constexpr int kDecFlatMaxB = 2048;      // sequences the flattened path supports (prefix array in shared memory)
-constexpr int kDecFlatMaxCtas = 320;    // upper bound of its grid (two CTAs per SM)
 // Tiles a warp asks for before the wait of an overlapped launch.  Against 3: 2 are 1.008x for 16 sequences over 4224 slots and
 // 0.996x for short caches, 5 are 0.988x and 1.000x (what is asked for competes with the tail of the step before).
 constexpr int kDecHintTiles = 3;
@@ -550,10 +549,11 @@ __global__ void __launch_bounds__(kDecWarps * 32) decode_stream_kernel(const Dec
     // record (its stores are ordered before by the barrier) and acquires the others'.
     __syncthreads();
     if (threadIdx.x == 0) {
-      const unsigned ticket = ticket_add(a.unit_count + u);
+      unsigned int* count = unit_counter(a.unit_count, a.B * ups, static_cast<int>(u), c_lo);
+      const unsigned ticket = ticket_add(count);
       const bool last = ticket + 1u == static_cast<unsigned>(pieces);
       s_last = last;
-      if (last) a.unit_count[u] = 0u;
+      if (last) *count = 0u;
     }
     __syncthreads();
     if (s_last) decode_merge_unit<D>(a, reinterpret_cast<float*>(dsmem), b, k, u, c_lo, c_hi - c_lo + 1, total, gridDim.x);
@@ -733,11 +733,10 @@ size_t lg_sparse_decode_workspace_bytes(const lg_decode_params* p) {
   if (decode_is_flat(p)) {   // one record per (CTA, unit) pair that can occur: index CTA + unit
     const int HG = (p->Hq / p->Hkv + kDecHeads - 1) / kDecHeads;
     const size_t units = static_cast<size_t>(p->B) * p->Hkv * HG;
-    const size_t records = static_cast<size_t>(kDecFlatMaxCtas) + units;
-    return sizeof(WsHeader) + align_up(units * sizeof(unsigned int), 256) +
-           align_up(records * kDecHeads * (p->D + 2) * sizeof(float), 256);
+    const size_t records = static_cast<size_t>(kDecMaxCtas) + units;
+    return kDecRecordOffset + align_up(records * kDecHeads * (p->D + 2) * sizeof(float), 256);
   }
-  return sizeof(WsHeader) + align_up(decode_part_bytes(p, choose_nsplit(p)), 256);
+  return kDecRecordOffset + align_up(decode_part_bytes(p, choose_nsplit(p)), 256);
 }
 
 lg_status lg_sparse_decode_workspace_init(void* workspace, size_t workspace_bytes, void* stream) {
@@ -767,7 +766,8 @@ lg_status lg_sparse_decode(const lg_decode_params* p, const void* q, const void*
   a.k_cache = static_cast<const __nv_bfloat16*>(k_cache);
   a.v_cache = static_cast<const __nv_bfloat16*>(v_cache);
   a.n_tokens = n_tokens;
-  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + sizeof(WsHeader));
+  a.unit_count = reinterpret_cast<unsigned int*>(static_cast<uint8_t*>(workspace) + kDecCountOffset);
+  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kDecRecordOffset);
   a.o = static_cast<__nv_bfloat16*>(o);
   a.lse = lse;
   a.Hq = p->Hq; a.Hkv = p->Hkv; a.G = p->Hq / p->Hkv;
@@ -788,18 +788,15 @@ lg_status lg_sparse_decode(const lg_decode_params* p, const void* q, const void*
     const int64_t pipe_bytes = static_cast<int64_t>(kDecWarps) * kDecStages * 2 * kDecTile * p->D * 2;
     const int per_sm = pipe_bytes * 2 + 4096 <= 227 * 1024 ? 2 : 1;
     if (n_cta > per_sm * sms) n_cta = per_sm * sms;
-    if (n_cta > kDecFlatMaxCtas) n_cta = kDecFlatMaxCtas;
+    if (n_cta > kDecMaxCtas) n_cta = kDecMaxCtas;
     // A whole number of CTAs per unit when that costs at most a quarter of the CTAs: with equal
     // lengths every slice then lies inside one unit (one pipeline fill, one record, one ticket per
     // CTA instead of two); with mixed lengths the slices fall where they fall, as before.
     if (units > 0 && n_cta > units && (n_cta / units) * units * 4 >= n_cta * 3) n_cta = (n_cta / units) * units;
     if (n_cta < 1) n_cta = 1;
     if (units > 0x7fffffff) return LG_ERR_UNSUPPORTED;
-    // header word and per-unit counters are zero on entry (the caller zero-filled the workspace once,
-    // and the CTA that merges a unit re-arms its counter); the records follow them
-    const size_t count_bytes = align_up(static_cast<size_t>(units) * sizeof(unsigned int), 256);
-    a.unit_count = reinterpret_cast<unsigned int*>(static_cast<uint8_t*>(workspace) + sizeof(WsHeader));
-    a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + sizeof(WsHeader) + count_bytes);
+    // header word and counters are zero on entry (the caller zero-filled the workspace once, and the CTA that merges a unit
+    // re-arms its counter)
     const int smem_flat = kDecWarps * kDecStages * 2 * kDecTile * p->D * 2 + (p->B + 1) * static_cast<int>(sizeof(int));
     return launch_kernel(true, p->D == 128 ? decode_stream_kernel<128> : decode_stream_kernel<64>, dim3(static_cast<unsigned>(n_cta)),
                              kDecWarps * 32, smem_flat, st, a) == cudaSuccess ? LG_OK : LG_ERR_CUDA;

@@ -25,3 +25,8 @@ def check_growth(size, D):
 def test_paged(lib, D):
     check_growth(lambda B, d: lib.lg_paged_decode_workspace_bytes(C.byref(
         binding.paged_params(B, 64, 8, d, 128, 4096, page_tokens=64, num_pages=100))), D)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_ring(lib, D):
+    check_growth(lambda B, d: lib.lg_sparse_decode_workspace_bytes(C.byref(binding.decode_params(B, 64, 8, d, 128, 4096))), D)

@@ -51,3 +51,46 @@ def test_paged_decode(lg):
         (9, 64, 8, 128, 2048, [2048 - b for b in range(9)]), (7, 16, 2, 64, 2048, uneven), (1, 16, 2, 64, 2048, [2000]), (40, 64, 8, 64, 2048, [2048] * 40),
         (7, 16, 2, 64, 2048, uneven), (50, 64, 8, 128, 640, [640] * 50), (3, 24, 2, 128, 2048, [2048, 700, 1]), (9, 64, 8, 128, 2048, [2048] * 9),
     ], lg.paged_decode_workspace)
+
+
+def ring(lg, B, Hq, Hkv, D, window, n):
+    p = lg.decode_params(B, Hq, Hkv, D, 0, window)
+    k, v = (randn(B, Hkv, window, D, seed=s).bfloat16() for s in (1, 2))
+    q, counts = randn(B, Hq, D, seed=3).bfloat16(), torch.tensor(n, dtype=torch.int64, device="cuda")
+    return p, lambda o, lse, ws: lg.lg_sparse_decode(p, q, k, v, counts, o=o, lse=lse, workspace=ws)
+
+
+# rings of 2048 tokens; (B, Hq, Hkv, D, window, n): few sequences, more of them, other head counts and dimensions, many units, and
+# (2100 sequences) the schedule that needs no counters
+RINGS = [
+    (1, 64, 8, 128, 2048, [2048]), (9, 64, 8, 128, 2048, [2048] * 9), (8, 64, 8, 128, 2048, [5000] * 8), (16, 64, 8, 128, 2048, [2048] * 16),
+    (2100, 1, 1, 64, 32, [20] * 2100), (9, 64, 8, 128, 2048, [2048 - b for b in range(9)]), (7, 16, 2, 64, 2048, [2048, 1, 0, 700, 2000, 64, 17]),
+    (1, 16, 2, 64, 2048, [2000]), (40, 64, 8, 64, 2048, [2048] * 40), (50, 64, 8, 128, 640, [640] * 50), (9, 64, 8, 128, 2048, [2048] * 9),
+]
+
+
+def test_ring_decode(lg):
+    check_in_turn(lg, ring, RINGS, lg.decode_workspace)
+
+
+def test_decode_of_the_fixed_array(lg):
+    """The same in turn over the array of the library, which every call of the process shares."""
+    for c in RINGS:
+        p, run = ring(lg, *c)
+        if lg.decode_workspace(p).numel() > lg.DECODE_STATIC_SCRATCH_BYTES:
+            continue
+        q, k, v = randn(p.B, p.Hq, p.D, seed=3).bfloat16(), *(randn(p.B, p.Hkv, c[4], p.D, seed=s).bfloat16() for s in (1, 2))
+        n = torch.tensor(c[5], dtype=torch.int64, device="cuda")
+        o, lse = torch.full_like(q, 7.0), torch.full((p.B, p.Hq), 7.0, device="cuda")
+        want, want_lse = torch.empty_like(o), torch.empty_like(lse)
+        lg.lg_sparse_decode_static(p, q, k, v, n, o, lse)
+        run(want, want_lse, lg.decode_workspace(p))
+        assert torch.equal(o, want) and torch.equal(lse, want_lse), c[:5]
+
+
+def test_both_caches(lg):
+    """Calls over the ring and over pages on one workspace."""
+    check_in_turn(lg, lambda lg, make, *c: make(lg, *c), [
+        (ring, 1, 64, 8, 128, 2048, [2048]), (paged, 9, 64, 8, 128, 2048, [2048] * 9), (paged, 1, 64, 8, 128, 2048, [2048]),
+        (ring, 9, 64, 8, 128, 2048, [2048] * 9), (paged, 40, 64, 8, 64, 1024, [1024] * 40), (ring, 40, 64, 8, 64, 1024, [1024] * 40),
+    ], lambda p: lg.paged_decode_workspace(p) if isinstance(p, lg.PagedParams) else lg.decode_workspace(p))
