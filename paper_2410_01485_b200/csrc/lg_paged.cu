@@ -1332,7 +1332,7 @@ lg_status lg_paged_append(const lg_paged_params* p, void* k_pool, void* v_pool, 
   a.stride_t = p->D;
   a.stride_h = static_cast<int64_t>(T_new) * p->D;
   a.stride_b = a.stride_h * p->Hkv;
-  if (new_strides && (new_strides[0] || new_strides[1] || new_strides[2])) {
+  if (new_strides) {
     for (int i = 0; i < 3; ++i)
       if (new_strides[i] <= 0 || new_strides[i] % 8 != 0) return LG_ERR_INVALID_ARG;
     a.stride_b = new_strides[0]; a.stride_h = new_strides[1]; a.stride_t = new_strides[2];
