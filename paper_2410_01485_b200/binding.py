@@ -140,6 +140,8 @@ def _set_strides(p: AttnParams, q, k, v, o):
     qs, ks, vs, os_ = q.stride(), k.stride(), v.stride(), o.stride()
     assert len(qs) == len(ks) == len(vs) == len(os_) == 4 and qs[3] == ks[3] == vs[3] == os_[3] == 1, \
         "expect [B, H, L, D] with contiguous D"
+    for t, s in ((q, qs), (k, ks), (v, vs), (o, os_)):     # (the library takes three zeros for a contiguous tensor)
+        assert s[0] or s[1] or s[2] or t.is_contiguous(), "expect q, k, v, o not broadcast over B, H and L at once"
     _pack_strides(p, _STRIDES_AT, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], os_[0], os_[1], os_[2])
     return qs, ks, vs, os_
 
