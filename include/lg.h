@@ -422,8 +422,9 @@ lg_status lg_paged_gather(const lg_paged_params* p, const void* k_pool, const vo
 
 /* lg_sparse_decode over the paged cache: q [B,Hq,D], o [B,Hq,D] bf16, lse [B,Hq] fp32 (NULL to skip), n_tokens (device
  * int64 [B]) counts the tokens appended so far, the current one included.  Scores and outputs are computed from the codes
- * without further rounding of K, V or q (but for elements of a row of q below 2^-24 of its largest); the weights are
- * rounded to f16, their sum is not.  workspace: device, 256-byte aligned, lg_paged_decode_workspace_bytes() bytes (0 = invalid
+ * without further rounding of K, V or q (but for elements of a row of q below 2^-24 of its largest); the weights, each
+ * times its page's V scale, are rounded to f16, their sum is not: below 2^-25 of the largest they lose bits, below 2^-36 they
+ * count as nothing in o (2^-19 and 2^-30 where the V scales of a sequence differ).  workspace: device, 256-byte aligned, lg_paged_decode_workspace_bytes() bytes (0 = invalid
  * arguments), zero-filled once by lg_sparse_decode_workspace_init(); one that is large enough for several calls serves them in
  * turn, whatever their sizes; two calls that can run at the same time (two captured graphs too) need a workspace each.   */
 size_t lg_paged_decode_workspace_bytes(const lg_paged_params* p);

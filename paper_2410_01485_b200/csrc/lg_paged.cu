@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const Gath
 // (K as e4m3 in products of its own kind, with q as the sum of two e4m3 numbers, needs no conversion but was slower: one sequence over 4224
 // slots 14.0 us against 12.4 with its append, 16 over 60-131 thousand 531 us against 500.)
 // A page's K scale multiplies its scores; that of V goes into the weights, w_j = p_j vs / vs_ref with the largest scale of the unit so far, so that
-// they fit f16 (11 bits down to 2^-14), while the row sum is kept in fp32.  Where the scales of a unit's pages lie more than 2^6 apart that would
+// they fit f16 (kWeightTop), while the row sum is kept in fp32.  Where the scales of a unit's pages lie more than 2^6 apart that would
 // cost bits, and the weights get a running reference of their own, w_j = 2^(s_j + log2 vs - r).
 // The instructions of a tile count although HBM bounds the kernel: in a loop of milliseconds the board is at its power limit, and the clock
 // that it takes back is the SMs' (16 sequences over 60-131 thousand slots, 600 steps in a row: 521 us with a maximum and a rescaling in every
@@ -426,6 +426,11 @@ constexpr int kPagedMaxB = 4096;        // sequences of one launch (their prefix
 //   several             1 x 8 x 4224 12.4 | 11.2, 1 x 4 x 8192 13.6 | 11.2, 4 x 8 x 4224 16.3 | 15.2, 9 x 8 x 4224 22.5 | 21.3
 //   several units a CTA, if alike   32 x 8 x 4224 58.4 | 56.1, 200 x 8 x 1024 94.2 | 90.3
 constexpr uint32_t kMergeTiles = 16;
+// The weights' place in f16, log2: they stay below 2^kWeightTop (f16 ends just under 2^16), and a reference that moves puts the maximum at
+// 2^kWeightMax.  The row sum counts weights that an f16 of theirs drops, and beside one large weight (a sink's) there may be 10^5 of them: so the
+// maximum lies high, not at 1, and they keep 11 bits down to 2^-25 of it and something down to 2^-36.  The room above spares moves: maximum at 2^7 | 2^11 |
+// 2^13, 1 and 16 sequences over 4224 slots 11.16 32.2 | 11.15 32.2 | 11.15 32.4 us with their append, 48 small ones 12.6 | 12.6 | 12.7.
+constexpr float kWeightTop = 15.f, kWeightMax = 11.f;
 constexpr float kNoScore = -3.4e38f;    // the reference of a row that has attended nothing
 
 struct PagedDecodeArgs {
@@ -974,12 +979,11 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
     bool moved = false;
     scores(m_run[0], m_run[1]);
     top();
-    // The reference moves to the maximum when a probability passes 2^8; until then fp32 sums and f16 weights (up to 2^15) do without.
-    if (__any_sync(0xffffffffu, fmaxf(t0, t1) > 8.f)) {
+    if (__any_sync(0xffffffffu, fmaxf(t0, t1) > kWeightTop)) {
       scores(0.f, 0.f);
       top();
       over_tokens();
-      t0 = fmaxf(m_run[0], t0); t1 = fmaxf(m_run[1], t1);
+      t0 = fmaxf(m_run[0], t0 - kWeightMax); t1 = fmaxf(m_run[1], t1 - kWeightMax);
       const float al0 = fast_exp2(m_run[0] - t0), al1 = fast_exp2(m_run[1] - t1);
       m_run[0] = t0; m_run[1] = t1;
       l_run[0] *= al0; l_run[1] *= al1;
@@ -1019,7 +1023,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
       for (int y = 0; y < 4; ++y) { w[0][y] += lv0; w[1][y] += lv1; }
       top();
       over_tokens();
-      t0 = fmaxf(r_run[0], t0); t1 = fmaxf(r_run[1], t1);
+      t0 = fmaxf(r_run[0], t0 - kWeightTop); t1 = fmaxf(r_run[1], t1 - kWeightTop);
       be0 *= fast_exp2(r_run[0] - t0); be1 *= fast_exp2(r_run[1] - t1);
       r_run[0] = t0; r_run[1] = t1;
       moved = true;

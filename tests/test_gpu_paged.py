@@ -777,3 +777,40 @@ def test_marshalled_calls(lg):
         s.ref.append(b, s.n[b], np64(k)[b], np64(v)[b])
     s.same_state()
     s.check_decode(q, o, lse, [41, 301])
+
+
+@pytest.mark.parametrize("place", ["first", "last"])
+@pytest.mark.parametrize("spread", [False, True])
+@pytest.mark.parametrize("below", [24.6, 26.0])
+def test_decode_many_small_weights_beside_a_large_one(lg, below, spread, place):
+    """A token whose score is far above all others and whose V is zero, before or behind 131072 tokens of weights 2^-below that agree: what o holds is
+    theirs alone.  A sequence for every warp, so that one warp works all of it; few pages, read again and again.  spread: one of the
+    pages has a V scale 2^9 times the others'.
+
+    Bound: as they stand relative to the large one, at 2^11, the weights are 2^-15 at least, where an f16 (steps of 2^-24) is off by up to 2^-10 of
+    it; o is rounded to bf16 (2^-8); the fp32 sums of weights and of products run over n / 16 steps and the merges, (n / 16 + 64) 2^-23 each
+    as everywhere here; 2^-14 for scores and exponentials.  What an f16 drops does not add up with n.  LSE: the sum's own error.
+    """
+    B, P, D, n = 1184, 128, 128, 131072
+    p = lg.paged_params(B, 1, 1, D, 0, n + P, page_tokens=P, num_pages=4, scale=math.log(2.0) * below)
+    k = torch.zeros(4, 1, P, D, device="cuda")
+    v = torch.ones(4, 1, P, D, device="cuda")
+    k[0, 0, 5, 0] = 1.0                                           # page 0: the large one at offset 5, alone or with others
+    v[0, 0, 5] = 0.0
+    v[2] = 2.0 ** -9                                              # page 2: under its larger scale the same as page 1
+    table = torch.full((B, n // P + 1), 1, dtype=torch.int32, device="cuda")
+    table[:, 0 if place == "first" else -1] = 0
+    if spread:
+        table[:, 600] = 2
+    scale = torch.ones(4, 1, device="cuda")
+    v_scale = scale.clone()
+    v_scale[2] = 2.0 ** 9
+    q = torch.zeros(B, 1, D, dtype=torch.bfloat16, device="cuda")
+    q[:, 0, 0] = 1.0
+    counts = torch.full((B,), n + P, dtype=torch.int64, device="cuda")
+    o, lse = lg.lg_paged_decode(p, q, k.to(F8), v.to(F8), scale, v_scale, table, counts)
+    tail = (n + P - 1) * 2.0 ** -below
+    want = tail / (1 + tail)
+    chain = (n / 16 + 64) * 2.0 ** -23
+    assert np.abs(np64(o) - want).max() <= want * (2.0 ** -8 + 2.0 ** -10 + 2 * chain + 2.0 ** -14)
+    assert np.abs(np64(lse) - (math.log(2.0) * below + math.log1p(tail))).max() <= chain + 2.0 ** -14
