@@ -445,6 +445,15 @@ __global__ void __launch_bounds__(kGatherThreads) chunk_prepare_kernel(const Sch
   }
 }
 
+// Where a call works its sequences in several runs: all its tables ahead of the first, so that one missing entry leaves every result unwritten.
+__global__ void __launch_bounds__(kGatherThreads) chunk_check_kernel(const PagedLinearise l, WsHeader* header, int begin) {
+  pdl_trigger();
+  pdl_wait();
+  if (begin && threadIdx.x == 0) header_begin(header);
+  const bool missing = paged_entry_missing(l, kGatherThreads);
+  if (missing && threadIdx.x == 0) atomicCAS(l.error_word, 0u, kPageError);
+}
+
 // ---- self-test of the bounded wait -----------------------------------------------------------
 // One thread waits on a barrier nobody will ever arrive at, with a limit of about a millisecond:
 // the wait gives up, records its site in the error word and the kernel ends normally.
@@ -777,6 +786,26 @@ lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   const int stride = paged_table_stride(p);
+  const int64_t cap = static_cast<int64_t>(p->sink_tokens) + p->window_tokens;
+  auto cache_of = [&](int x, int n_seq, int kept) {                 // what a launch over sequences x .. x + n_seq - 1 asks of the cache
+    PagedLinearise l{};
+    l.pool[0] = k_pool; l.pool[1] = v_pool; l.scale[0] = k_scale; l.scale[1] = v_scale;
+    l.error_word = reinterpret_cast<unsigned int*>(ws);
+    l.B = n_seq; l.Hkv = p->Hkv; l.D = p->D; l.T = T; l.kept = kept; l.sink = p->sink_tokens; l.window = p->window_tokens;
+    l.page_shift = page_shift(p->page_tokens); l.num_pages = p->num_pages; l.stride = stride;
+    l.table = block_table + static_cast<int64_t>(x) * stride;
+    for (int y = 0; y < n_seq; ++y) l.seq[y].held = static_cast<int>(n_tokens_before[x + y] < cap ? n_tokens_before[x + y] : cap);
+    return l;
+  };
+  const bool several = chunk_run(p, T, n_tokens_before, 0).end < p->B;
+  for (int x = 0; several && x < p->B; x += kLineariseSeqs) {
+    const int n_seq = p->B - x < kLineariseSeqs ? p->B - x : kLineariseSeqs;
+    int most = 0;
+    for (int y = 0; y < n_seq; ++y) most = n_tokens_before[x + y] < most ? most : static_cast<int>(n_tokens_before[x + y] < cap ? n_tokens_before[x + y] : cap);
+    if (launch_kernel(true, chunk_check_kernel, dim3(1), kGatherThreads, 0, st, cache_of(x, n_seq, most), reinterpret_cast<WsHeader*>(ws), x == 0 ? 1 : 0) !=
+        cudaSuccess)
+      return LG_ERR_CUDA;
+  }
   for (int b = 0; b < p->B;) {
     const ChunkRun run = chunk_run(p, T, n_tokens_before, b);
     const int e = run.end;
@@ -787,26 +816,19 @@ lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, 
     ChunkView* views = reinterpret_cast<ChunkView*>(ws + o_views);
     c.r.views = views;
     const bool own = !c.r.shared_lists;
-    if (!own && (s = prepare_workspace(c.r, c.w, ws, 1, true, 0, st)) != LG_OK) return s;
+    if (!own && (s = prepare_workspace(c.r, c.w, ws, 1, !several, 0, st)) != LG_OK) return s;
     SchedArgs sched{};
     sched.p = c.r.pat;
     sched.header = reinterpret_cast<WsHeader*>(ws);
     sched.R = 128 / c.r.block;
     sched.n_stiles = c.r.n_stiles; sched.st_row0 = c.r.st_row0;
-    PagedLinearise l;
-    l.pool[0] = k_pool; l.pool[1] = v_pool; l.scale[0] = k_scale; l.scale[1] = v_scale;
-    l.error_word = reinterpret_cast<unsigned int*>(ws);
-    l.Hkv = p->Hkv; l.D = p->D; l.T = T; l.kept = c.kept; l.sink = p->sink_tokens; l.window = p->window_tokens;
-    l.page_shift = page_shift(p->page_tokens); l.num_pages = p->num_pages; l.stride = stride;
     __nv_bfloat16* lin[2] = {reinterpret_cast<__nv_bfloat16*>(ws + c.o_k), reinterpret_cast<__nv_bfloat16*>(ws + c.o_v)};
     for (int x = b; x < e; x += kLineariseSeqs) {
-      l.B = e - x < kLineariseSeqs ? e - x : kLineariseSeqs;
-      const int64_t cap = static_cast<int64_t>(p->sink_tokens) + p->window_tokens;
+      PagedLinearise l = cache_of(x, e - x < kLineariseSeqs ? e - x : kLineariseSeqs, c.kept);
       const int bt = p->block_tokens;
       for (int y = 0; y < l.B; ++y) {
         const int64_t n = n_tokens_before[x + y];
         ChunkSeq& sq = l.seq[y];
-        sq.held = static_cast<int>(n < cap ? n : cap);
         sq.ring0 = static_cast<int>((n - sq.held) % p->window_tokens);
         sq.phase = bt > 0 ? static_cast<int>(((n - c.kept) % bt + bt) % bt) : 0;
         // the chunk's first token sees the furthest back: rows v with (kept + phase) / block - (v + phase) / block < window / block, or the last `window`
@@ -816,7 +838,6 @@ lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, 
         l.chunk[y] = static_cast<const __nv_bfloat16*>(y ? v_chunk : k_chunk) + static_cast<int64_t>(x) * p->Hkv * T * p->D;
         l.lin[y] = lin[y] + static_cast<int64_t>(x - b) * p->Hkv * c.ap.L * p->D;
       }
-      l.table = block_table + static_cast<int64_t>(x) * stride;
       sched.sq_order = reinterpret_cast<TileRec*>(ws + c.w.sq_order) + static_cast<int64_t>(x - b) * c.r.n_stiles;
       sched.sq_ent = reinterpret_cast<int32_t*>(ws + c.w.sq_ent) + (x - b) * c.r.ent_stride;
       const int64_t blocks_x = (static_cast<int64_t>(c.ap.L) * (p->D / 16) + kGatherThreads - 1) / kGatherThreads;
@@ -824,7 +845,7 @@ lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, 
       const int64_t blocks = blocks_x * p->Hkv * l.B + 1 + lists;
       if (blocks > 0x7fffffff) return LG_ERR_UNSUPPORTED;
       if (launch_kernel(true, chunk_prepare_kernel, dim3(static_cast<unsigned>(blocks)), kGatherThreads, 0, st, sched, l, views + (x - b),
-                        c.r.ent_stride, static_cast<int>(blocks_x), lists, own && x == b ? 1 : 0) != cudaSuccess)
+                        c.r.ent_stride, static_cast<int>(blocks_x), lists, own && !several && x == b ? 1 : 0) != cudaSuccess)
         return LG_ERR_CUDA;
     }
     if ((s = launch_fwd(c.r, c.w, static_cast<const __nv_bfloat16*>(q_chunk) + q_at * p->D, lin[0], lin[1],

@@ -814,3 +814,28 @@ def test_decode_many_small_weights_beside_a_large_one(lg, below, spread, place):
     chain = (n / 16 + 64) * 2.0 ** -23
     assert np.abs(np64(o) - want).max() <= want * (2.0 ** -8 + 2.0 ** -10 + 2 * chain + 2.0 ** -14)
     assert np.abs(np64(lse) - (math.log(2.0) * below + math.log1p(tail))).max() <= chain + 2.0 ** -14
+
+
+@pytest.mark.parametrize("n, T, sink", [([10, 100, 3, 400], 70, 64), ([90, 30], 16400, 0), ([3 + 100 * (b % 2) for b in range(140)], 70, 64)],
+                         ids=["sinks", "long", "B140"])
+@pytest.mark.parametrize("at", [0, -1])
+def test_chunk_of_several_runs_with_an_absent_page_writes_nothing(lg, n, T, sink, at):
+    """Sequences that are not worked together: a missing entry of the first or of the last leaves the others' results unwritten too."""
+    B = len(n)
+    s = Setup(lg, n, 1, 1, 64, sink, 64, 16)
+    q, k, v = randn(B, 1, T, 64, seed=1), randn(B, 1, T, 64, seed=2), randn(B, 1, T, 64, seed=3)
+    ws = lg.paged_chunk_prefill_workspace(s.p, T, n)
+    clean = lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n, workspace=ws)
+    assert lg.lg_last_status(ws) == 0
+    _check_chunk_rows(s, n[:2], T, q, k, v, *clean, [0, T - 1], [0])
+    good, s.ref.table = s.ref.table.copy(), s.ref.table.copy()
+    s.ref.table[at, 0] = s.num_pages
+    s.upload()
+    o, lse = torch.full_like(q, 7.0), torch.full((B, 1, T), 7.0, device="cuda")
+    lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n, o=o, lse=lse, workspace=ws)
+    assert lg.lg_last_status(ws) == -7
+    assert (o == 7).all() and (lse == 7).all()
+    s.ref.table = good
+    s.upload()
+    lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n, o=o, lse=lse, workspace=ws)
+    assert lg.lg_last_status(ws) == 0 and torch.equal(o, clean[0]) and torch.equal(lse, clean[1])
