@@ -100,7 +100,7 @@ struct FwdJoin {
 // Rows r0, r0 + step, .. below `end` of a tile of up to N pieces, kBatch of them at a time: a load from another SM takes 1000
 // cycles, so that one row after the other the share of a CTA took 6-8 us (4 heads x 3318 tokens, full causal, D = 128, two
 // pieces a tile: 45.1 us, in batches 41.1).
-template <int D, int N, int kBatch>
+template <int D, int N, int kBatch, bool kPaged>
 __device__ __forceinline__ void fwd_join_rows(const FwdArgs& a, uint32_t base, int n_segs, int b, int h, int row0, int r0, int end, int step, int c) {
   for (; r0 < end; r0 += kBatch * step) {
     float2 pair[kBatch][N];
@@ -136,12 +136,13 @@ __device__ __forceinline__ void fwd_join_rows(const FwdArgs& a, uint32_t base, i
       if (r < end && q < a.L && q >= a.q_start) {
         *reinterpret_cast<uint2*>(a.o + b * a.o_strides[0] + h * a.o_strides[1] + static_cast<int64_t>(q - a.q_start) * a.o_strides[2] + c * 4) =
             make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-        if (c == 0) a.lse[(static_cast<int64_t>(b) * a.Hq + h) * a.Lq + q - a.q_start] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        const bool some = kPaged ? l != 0.f : l > 0.f;            // (kPaged: a sum that is NaN stays NaN, as in a tile that is not cut)
+        if (c == 0) a.lse[(static_cast<int64_t>(b) * a.Hq + h) * a.Lq + q - a.q_start] = some ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
     }
   }
 }
-template <int D>
+template <int D, bool kPaged>
 __device__ __forceinline__ void fwd_join(const FwdArgs& a, uint32_t base, uint32_t failed_flag, int seg, int n_segs, int b, int h, int row0) {
   constexpr int kLanes = D / 4, kRows = 32 / kLanes;              // lanes of a row (four columns each), rows of a warp
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane % kLanes;
@@ -149,9 +150,9 @@ __device__ __forceinline__ void fwd_join(const FwdArgs& a, uint32_t base, uint32
   for (int i = 0; i < n_segs; ++i) failed |= cluster_ld32(cluster_addr(failed_flag, i));
   if (failed) return;                                             // a piece was given up: the status word says so
   const int first = 256 * seg / n_segs + warp * kRows + lane / kLanes, end = 256 * (seg + 1) / n_segs, step = kFwdThreads / 32 * kRows;
-  if (n_segs <= 2) fwd_join_rows<D, 2, 6>(a, base, n_segs, b, h, row0, first, end, step, c);
-  else if (n_segs <= 4) fwd_join_rows<D, 4, 4>(a, base, n_segs, b, h, row0, first, end, step, c);
-  else fwd_join_rows<D, 8, 2>(a, base, n_segs, b, h, row0, first, end, step, c);
+  if (n_segs <= 2) fwd_join_rows<D, 2, 6, kPaged>(a, base, n_segs, b, h, row0, first, end, step, c);
+  else if (n_segs <= 4) fwd_join_rows<D, 4, 4, kPaged>(a, base, n_segs, b, h, row0, first, end, step, c);
+  else fwd_join_rows<D, 8, 2, kPaged>(a, base, n_segs, b, h, row0, first, end, step, c);
 }
 
 // kPaged: a chunk over the paged cache.  Its sequences have their own lists and views, and O is divided by the sum of the probabilities as they
@@ -606,7 +607,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUt
         tc_fence_before();
       }
       cluster_sync();                                      // (threads of CTAs that have left are not waited for)
-      fwd_join<D>(a, smem_u32(smem), smem_u32(tmem_slot + 2), seg, n_segs, b, h, row0);
+      fwd_join<D, kPaged>(a, smem_u32(smem), smem_u32(tmem_slot + 2), seg, n_segs, b, h, row0);
       cluster_sync();                                      // nobody leaves while its sums are being read
     }
   }

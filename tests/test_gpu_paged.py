@@ -839,3 +839,17 @@ def test_chunk_of_several_runs_with_an_absent_page_writes_nothing(lg, n, T, sink
     s.upload()
     lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n, o=o, lse=lse, workspace=ws)
     assert lg.lg_last_status(ws) == 0 and torch.equal(o, clean[0]) and torch.equal(lse, clean[1])
+
+
+@pytest.mark.parametrize("D, window", [(128, 2048), (64, 2048), (128, 64)])
+def test_chunk_row_that_is_nan(lg, D, window):
+    """A NaN in one row of q is in that row's o and lse, and in no other's, whether the row's tile is cut along its keys (the long windows) or not."""
+    n, T = [3000], 33
+    s = Setup(lg, n, 2, 1, D, 128, window, 64)
+    q, k, v = randn(1, 2, T, D, seed=1), randn(1, 1, T, D, seed=2), randn(1, 1, T, D, seed=3)
+    clean = lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n)
+    q[0, 1, 5, 7] = float("nan")
+    o, lse = lg.lg_paged_chunk_prefill(s.p, q, k, v, *s.cache, s.table, n)
+    assert torch.isnan(o[0, 1, 5]).all() and torch.isnan(lse[0, 1, 5])
+    _check_chunk_rows(s, n, T, q, k, v, o, lse, [0, 4, 6, T - 1], [0, 1])
+    assert torch.equal(o[0, 0], clean[0][0, 0]) and torch.equal(lse[0, 0], clean[1][0, 0])
