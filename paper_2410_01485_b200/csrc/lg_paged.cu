@@ -477,6 +477,12 @@ __device__ __forceinline__ float fast_log2(float x) {   // (exact for the powers
   return y;
 }
 
+__device__ __forceinline__ float min_nan(float a, float b) {   // the smaller one; NaN if either is
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 template <int D>
 struct PagedSmem {
   static constexpr int kSlot = kPagedTile * D;                          // K (or V) of a tile
@@ -974,6 +980,15 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
         t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, o));
       }
     };
+    // Scores relative to a reference that was taken from them.  Where fp32 holds them in steps of 2 and more (from 2^24 on) the reference is as coarse,
+    // and the largest score's weight may come out above the largest f16, hence the minimum.  The scores are rounded before the difference is
+    // taken: in one step with the product, whose unrounded value may be half a step below, it could come out as 0.
+    auto less = [&](float ref0, float ref1) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) w[x][y] = min_nan(w[x][y] - (y & 1 ? ref1 : ref0), kWeightTop);
+    };
     float be0 = 1.f, be1 = 1.f;               // what O is multiplied by
     const float was0 = m_run[0], was1 = m_run[1];
     bool moved = false;
@@ -988,7 +1003,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
       m_run[0] = t0; m_run[1] = t1;
       l_run[0] *= al0; l_run[1] *= al1;
       if (!own) { be0 = al0; be1 = al1; moved = true; }
-      scores(t0, t1);
+      less(t0, t1);
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x)
@@ -1027,11 +1042,11 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
       be0 *= fast_exp2(r_run[0] - t0); be1 *= fast_exp2(r_run[1] - t1);
       r_run[0] = t0; r_run[1] = t1;
       moved = true;
+      less(t0, t1);
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        w[x][0] = fast_exp2(w[x][0] - t0); w[x][1] = fast_exp2(w[x][1] - t1);
-        w[x][2] = fast_exp2(w[x][2] - t0); w[x][3] = fast_exp2(w[x][3] - t1);
-      }
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) w[x][y] = fast_exp2(w[x][y]);
     }
     if (moved) {
 #pragma unroll

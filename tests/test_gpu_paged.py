@@ -853,3 +853,33 @@ def test_chunk_row_that_is_nan(lg, D, window):
     assert torch.isnan(o[0, 1, 5]).all() and torch.isnan(lse[0, 1, 5])
     _check_chunk_rows(s, n, T, q, k, v, o, lse, [0, 4, 6, T - 1], [0, 1])
     assert torch.equal(o[0, 0], clean[0][0, 0]) and torch.equal(lse[0, 0], clean[1][0, 0])
+
+
+def _check_averages(lg, bits, spread):
+    """Scores of 2^bits, whose steps in fp32 are up to 2^11: o is an average of the V rows all the same, and the LSE that of the largest.
+
+    A score is off by 2^-19 scale sum |q k|, as everywhere here, and its roundings on the way to a weight (2^-22 of it): `step`.  What is 2 steps and 30 below
+    the largest has a weight below 2^-43; of the others any may have any weight.  o is rounded to bf16 (2^-8), weights to f16, which is not the sum's
+    share (2^-11), and what f16 drops or the others weigh is below 2^-30 each, V as large as it may be."""
+    n = [1024 - 7 * b for b in range(40)]
+    s = Setup(lg, n, 4, 4, 64, 0, 1024, 32, scales=(-spread, spread))
+    s.ref.scale[0][:] = 2.0 ** -7
+    s.upload()
+    q = (randn(40, 4, 64, seed=5).float() * 2.0 ** (bits - 1)).to(torch.bfloat16)
+    o, lse = lg.lg_paged_decode(s.p, q, *s.cache, s.table, s.counts())
+    assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+    for b in (0, 1, 39):
+        for h in range(4):
+            pos, k, v = s.ref.rows(b, h, n[b])
+            x = k @ np64(q[b, h]) / 8
+            step = 2.0 ** -19 * (np.abs(k) @ np.abs(np64(q[b, h]))).max() / 8 + 2.0 ** -22 * np.abs(x).max()
+            assert abs(lse[b, h].item() - x.max()) <= 2 * step + math.log(len(x)) + 2.0 ** -10
+            near = v[x >= x.max() - 2 * step - 30]
+            lo, hi = near.min(0), near.max(0)
+            slack = (2.0 ** -8 + 2.0 ** -10) * np.maximum(np.abs(lo), np.abs(hi)) + len(x) * 2.0 ** -30 * np.abs(v).max(0)
+            assert np.all(np64(o[b, h]) >= lo - slack) and np.all(np64(o[b, h]) <= hi + slack), (b, h)
+
+
+@pytest.mark.parametrize("bits", [14, 20, 23, 24, 25, 26, 27, 28, 29, 30, 34])
+def test_decode_scores_far_beyond_what_fp32_tells_apart(lg, bits):
+    _check_averages(lg, bits, 0)
