@@ -411,7 +411,8 @@ __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const Gath
 // slots 14.0 us against 12.4 with its append, 16 over 60-131 thousand 531 us against 500.)
 // A page's K scale multiplies its scores; that of V goes into the weights, w_j = p_j vs / vs_ref with the largest scale of the unit so far, so that
 // they fit f16 (kWeightTop), while the row sum is kept in fp32.  Where the scales of a unit's pages lie more than 2^6 apart that would
-// cost bits, and the weights get a running reference of their own, w_j = 2^(s_j + log2 vs - r).
+// cost bits, and the weights get a running reference of their own, w_j = 2^(s_j - m + log2 vs - r), r relative to the probabilities' m (log2 vs
+// added to a large score would be rounded away).
 // The instructions of a tile count although HBM bounds the kernel: in a loop of milliseconds the board is at its power limit, and the clock
 // that it takes back is the SMs' (16 sequences over 60-131 thousand slots, 600 steps in a row: 521 us with a maximum and a rescaling in every
 // tile and two exponentials a weight, 500 us so).
@@ -844,7 +845,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
   float oacc[D / 16][4];
   float vs_ref = -1.f, vs_inv = 0.f, vs_min = 0.f;   // largest V scale so far, its reciprocal, the smallest one
   bool own = false;                          // the V scales lie too far apart: the weights have a reference of their own
-  float r_run[2];                            // ... this one
+  float r_run[2];                            // ... this one (relative to m_run)
   int nvalid = 0, ex0 = 0, ex_cnt = 0, first_t = 0;
   const int ring_w = a.C - a.sink;
   auto attended = [&](int slot) {
@@ -1003,14 +1004,16 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
       m_run[0] = t0; m_run[1] = t1;
       l_run[0] *= al0; l_run[1] *= al1;
       if (!own) { be0 = al0; be1 = al1; moved = true; }
+      else { r_run[0] = fmaxf(r_run[0] + (was0 - t0), kNoScore); r_run[1] = fmaxf(r_run[1] + (was1 - t1), kNoScore); }
       less(t0, t1);
     }
+    float pr[2][4];
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
-      for (int y = 0; y < 4; ++y) w[x][y] = fast_exp2(w[x][y]);
-    l_run[0] += (w[0][0] + w[0][2]) + (w[1][0] + w[1][2]);
-    l_run[1] += (w[0][1] + w[0][3]) + (w[1][1] + w[1][3]);
+      for (int y = 0; y < 4; ++y) pr[x][y] = fast_exp2(w[x][y]);
+    l_run[0] += (pr[0][0] + pr[0][2]) + (pr[1][0] + pr[1][2]);
+    l_run[1] += (pr[0][1] + pr[0][3]) + (pr[1][1] + pr[1][3]);
     // The pages' V scales relative to the largest so far (a half that is not there has no weights).
     const float v0 = in0 ? sc.y : in1 ? sc.w : vs_ref, v1 = in1 ? sc.w : v0;
     if (!own && v0 > 0.f && (fmaxf(v0, v1) > vs_ref || fminf(v0, v1) < vs_min)) {
@@ -1019,7 +1022,8 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
       own = vs_min * 64.f < most;
       if (own) {                              // O keeps the reference that it had: what moved m may weigh little, having a small scale
         const float lr = fast_log2(vs_ref);
-        r_run[0] = vs_ref > 0.f ? was0 + lr : kNoScore; r_run[1] = vs_ref > 0.f ? was1 + lr : kNoScore;
+        r_run[0] = vs_ref > 0.f ? fmaxf(was0 - m_run[0] + lr, kNoScore) : kNoScore;
+        r_run[1] = vs_ref > 0.f ? fmaxf(was1 - m_run[1] + lr, kNoScore) : kNoScore;
         be0 = be1 = 1.f;
       } else if (most != vs_ref) {
         if (vs_ref > 0.f) { be0 *= vs_ref / most; be1 *= vs_ref / most; moved = true; }
@@ -1030,10 +1034,9 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
     if (!own) {
       const float h0 = v0 * vs_inv, h1 = v1 * vs_inv;
 #pragma unroll
-      for (int y = 0; y < 4; ++y) { w[0][y] *= h0; w[1][y] *= h1; }
+      for (int y = 0; y < 4; ++y) { w[0][y] = pr[0][y] * h0; w[1][y] = pr[1][y] * h1; }
     } else {
       const float lv0 = fast_log2(v0), lv1 = fast_log2(v1);
-      scores(0.f, 0.f);
 #pragma unroll
       for (int y = 0; y < 4; ++y) { w[0][y] += lv0; w[1][y] += lv1; }
       top();
@@ -1099,7 +1102,7 @@ __global__ void __launch_bounds__(kDecThreads, D == 64 ? 2 : 1) paged_decode_ker
       }
       float g[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) g[x] = own ? fast_exp2(r_run[x] - m_run[x]) : vs_ref;
+      for (int x = 0; x < 2; ++x) g[x] = own ? fast_exp2(r_run[x]) : vs_ref;
       if (first_t == 0 && tail) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {

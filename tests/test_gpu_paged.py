@@ -883,3 +883,9 @@ def _check_averages(lg, bits, spread):
 @pytest.mark.parametrize("bits", [14, 20, 23, 24, 25, 26, 27, 28, 29, 30, 34])
 def test_decode_scores_far_beyond_what_fp32_tells_apart(lg, bits):
     _check_averages(lg, bits, 0)
+
+
+@pytest.mark.parametrize("bits", [6, 12, 18, 20, 24, 28, 34])
+def test_decode_large_scores_over_scales_far_apart(lg, bits):
+    """V scales that differ by up to 2^40 beside scores that fp32 holds in large steps: a scale weighs what it is, not what is left of it beside a score."""
+    _check_averages(lg, bits, 20)
