@@ -440,10 +440,12 @@ lg_status lg_paged_decode(const lg_paged_params* p, const void* q, const void* k
  * but one token of its last block, where the window is block-aligned) beside a sequence that holds fewer than sink_tokens:
  * sequences that hold equally many should then be neighbours.)
  * sink_tokens and window_tokens are multiples of 64, window_tokens >= 64.  The cache is copied in bf16 and in time order
- * into the workspace (device, 256-byte aligned,
- * lg_paged_chunk_prefill_workspace_bytes() bytes), and the forward kernel runs over it.  As there, a V that is not finite
+ * into the workspace (device, 256-byte aligned, lg_paged_chunk_prefill_workspace_bytes() bytes: of the sequences that are
+ * worked together 4 D Hkv (h + T) bytes each, h the most tokens that one of them holds, which is twice the size of the
+ * cache itself, and some KB of lists), and the forward kernel runs over it.  As there, a V that is not finite
  * reaches every query whose tile holds its token, whether the query sees it or not (tokens that no query of the chunk sees
- * are left out).  A failure of any of the launches is reported by lg_last_status(workspace, stream).                   */
+ * are left out).  Whether a row of O is divided by the sum of its weights as they were rounded is decided for 32 rows at a
+ * time: a row's last bits may depend on its neighbours, the same ones every time.  A failure of any of the launches is reported by lg_last_status(workspace, stream).                   */
 size_t lg_paged_chunk_prefill_workspace_bytes(const lg_paged_params* p, int32_t T, const int64_t* n_tokens_before);
 lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, const void* k_chunk,
                                  const void* v_chunk, const void* k_pool, const void* v_pool, const float* k_scale,

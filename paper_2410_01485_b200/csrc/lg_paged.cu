@@ -408,14 +408,14 @@ __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const Gath
 // and V enter without rounding, and q (8 significant bits) does not lose any either once its row is scaled by a power of
 // two.  A contraction 8 heads wide is far below a tcgen05 tile.
 // (K as e4m3 in products of its own kind, with q as the sum of two e4m3 numbers, needs no conversion but was slower: one sequence over 4224
-// slots 14.0 us against 12.4 with its append, 16 over 60-131 thousand 531 us against 500.)
+// slots 14.0 us against 12.4 with its append, 16 over 60-131 thousand 1.06 times as long.)
 // A page's K scale multiplies its scores; that of V goes into the weights, w_j = p_j vs / vs_ref with the largest scale of the unit so far, so that
 // they fit f16 (kWeightTop), while the row sum is kept in fp32.  Where the scales of a unit's pages lie more than 2^6 apart that would
 // cost bits, and the weights get a running reference of their own, w_j = 2^(s_j - m + log2 vs - r), r relative to the probabilities' m (log2 vs
 // added to a large score would be rounded away).
-// The instructions of a tile count although HBM bounds the kernel: in a loop of milliseconds the board is at its power limit, and the clock
-// that it takes back is the SMs' (16 sequences over 60-131 thousand slots, 600 steps in a row: 521 us with a maximum and a rescaling in every
-// tile and two exponentials a weight, 500 us so).
+// The instructions of a tile count although HBM bounds the kernel: in a loop of tens of milliseconds the board is at its power limit, and the clock
+// that it takes back is the SMs'.  16 sequences over 60-131 thousand slots, 3.13 GB a step: 502 us (6.2 TB/s) at 1965 MHz, 518-522 us (6.0 TB/s) at the
+// 1580 MHz of thousands of steps in a row; there a maximum and a rescaling in every tile and two exponentials a weight cost 4 % more.
 constexpr int kPagedTile = 32, kPagedHalf = 16;   // tokens of a tile, and of what lies in one page whatever its size
 constexpr int kPagedSlots = 5;          // 4 KB each at D = 128: three tiles' K and two tiles' V, or the other way round
 constexpr int kPagedMaxB = 4096;        // sequences of one launch (their prefix sums lie in shared memory)
