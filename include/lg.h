@@ -424,9 +424,10 @@ lg_status lg_paged_gather(const lg_paged_params* p, const void* k_pool, const vo
  * int64 [B]) counts the tokens appended so far, the current one included.  Scores and outputs are computed from the codes
  * without further rounding of K, V or q (but for elements of a row of q below 2^-24 of its largest); the weights, each
  * times its page's V scale, are rounded to f16, their sum is not: below 2^-25 of the largest they lose bits, below 2^-36 they
- * count as nothing in o (2^-19 and 2^-30 where the V scales of a sequence differ).  workspace: device, 256-byte aligned, lg_paged_decode_workspace_bytes() bytes (0 = invalid
- * arguments), zero-filled once by lg_sparse_decode_workspace_init(); one that is large enough for several calls serves them in
- * turn, whatever their sizes; two calls that can run at the same time (two captured graphs too) need a workspace each.   */
+ * count as nothing in o (2^-19 and 2^-30 where the V scales of a sequence differ).  workspace: device, 256-byte aligned,
+ * lg_paged_decode_workspace_bytes() bytes (0 = invalid arguments), zero-filled once by lg_sparse_decode_workspace_init();
+ * one that is large enough for several calls serves them in turn, whatever their sizes; two calls that can run at the same
+ * time (two captured graphs too) need a workspace each.                                                              */
 size_t lg_paged_decode_workspace_bytes(const lg_paged_params* p);
 lg_status lg_paged_decode(const lg_paged_params* p, const void* q, const void* k_pool, const void* v_pool,
                           const float* k_scale, const float* v_scale, const int32_t* block_table,
@@ -445,7 +446,8 @@ lg_status lg_paged_decode(const lg_paged_params* p, const void* q, const void* k
  * cache itself, and some KB of lists), and the forward kernel runs over it.  As there, a V that is not finite
  * reaches every query whose tile holds its token, whether the query sees it or not (tokens that no query of the chunk sees
  * are left out).  Whether a row of O is divided by the sum of its weights as they were rounded is decided for 32 rows at a
- * time: a row's last bits may depend on its neighbours, the same ones every time.  A failure of any of the launches is reported by lg_last_status(workspace, stream).                   */
+ * time: a row's last bits may depend on its neighbours, the same ones every time.  A failure of any of the launches is
+ * reported by lg_last_status(workspace, stream).                                                                     */
 size_t lg_paged_chunk_prefill_workspace_bytes(const lg_paged_params* p, int32_t T, const int64_t* n_tokens_before);
 lg_status lg_paged_chunk_prefill(const lg_paged_params* p, const void* q_chunk, const void* k_chunk,
                                  const void* v_chunk, const void* k_pool, const void* v_pool, const float* k_scale,
